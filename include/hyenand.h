@@ -432,6 +432,94 @@ hyenand_status hyenand_modal_filter(const float* log_mag, const float* angle, co
                                     const float* res_im, int order, void* k, int64_t C, int64_t L, hyenand_dtype dtype,
                                     void* stream);
 
+/*
+ * hyenand_scan -- the gated linear recurrence along the last axis of [B, C, L]
+ * tensors: the mixer of hyenand_fftconv with a decay of its own at every
+ * position in place of the kernel.  For every sample b and channel c
+ *
+ *     u_t = x1_t * v_t                                      (inner gate)
+ *     h_t = exp(log_a_t) * h_{t-1} + u_t,  h_{-1} = h0[b,c]  (recurrence)
+ *     y_t = x2_t * (h_t + D[c] * u_t)                (shortcut, outer gate)
+ *
+ * With log_a constant along a row it is the linear long convolution with
+ * k_t = exp(t * log_a) (section "Background", the recurrence unrolled).
+ *
+ * x1, x2, v, log_a, y : device pointers, contiguous [B, C, L] of dtype, aligned
+ *   to their element; D: [C] of dtype.  log_a <= 0 keeps the state bounded; a
+ *   positive one grows and overflows where the product of the decays of some
+ *   span of positions does.  log_a below -87 (exp of it leaves fp32), -inf
+ *   among it, starts a new sequence: h_t = u_t, whatever came before, an
+ *   infinity or a NaN included.  Several sequences can so lie in one row.
+ * h0 (NULL: zeros), h_last (NULL: not written) : [B, C] fp32, the state before
+ *   the first position and behind the last one.  h_last may be h0 itself.
+ * lengths : [B] int64, or NULL for L everywhere.  Positions t >= lengths[b] are
+ *   not read, y there is 0, and h_last is the state behind position
+ *   lengths[b] - 1 (h0 for a length of 0).  A length below 0 counts as 0, one
+ *   above L as L.
+ * states : [B, C, ceil(L / HYENAND_SCAN_BLOCK)] fp32 or NULL: the state before
+ *   every position that is a multiple of HYENAND_SCAN_BLOCK (behind the sample's
+ *   end: its last one), which hyenand_scan_backward starts from.
+ * B * C < 2^22, L <= 2^40, B * C * L <= 2^46.
+ * workspace : at least hyenand_scan_workspace_size() bytes (0 for calls of many
+ *   rows), 16-byte aligned; owned by the caller, its contents overwritten.
+ * No output may overlap an input or another output, but for h_last = h0.
+ * The state, the decays and their products are fp32 in both storage types; the
+ * decay of a span is the exponential of a sum, so memories of any length lose no
+ * accuracy to the product of many factors.  Validation, stream and error
+ * conventions as for hyenand_fftconv; results are deterministic.
+ */
+#define HYENAND_SCAN_BLOCK 512
+hyenand_status hyenand_scan(const void* x1, const void* x2, const void* v, const void* log_a, const void* D,
+                            const float* h0, const int64_t* lengths, void* y, float* h_last, float* states, int64_t B,
+                            int64_t C, int64_t L, hyenand_dtype dtype, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* Workspace bytes that hyenand_scan takes.  Pure host function. */
+hyenand_status hyenand_scan_workspace_size(int64_t B, int64_t C, int64_t L, hyenand_dtype dtype, size_t* bytes_out);
+
+/*
+ * hyenand_scan_backward -- gradients of a scalar loss through hyenand_scan,
+ * given gy = dLoss/dy and (NULL: zeros) gh_last = dLoss/dh_last.  With
+ * gz = gy * x2 and c_t = exp(log_a_t) * gh_t:
+ *
+ *     gx2 = gy * (h + D u),  gh_t = gz_t + c_{t+1} (gz_t + gh_last at the end),
+ *     gx1 = (gh + D gz) v,   gv = (gh + D gz) x1,   glog_a_t = c_t h_{t-1},
+ *     gD[c] = sum over b and t of gz u,             gh0 = c_0
+ *
+ * Inputs, lengths and dtype are those of the forward call, states what it
+ * wrote (they hold h0).  gx1, gx2, gv, glog_a: [B, C, L] of dtype, 0 at t >=
+ * lengths[b] (gy is not read there); gD: [C] of dtype; gh0: [B, C] fp32 or NULL.
+ * Where a sequence starts, no gradient passes and glog_a is 0.
+ * workspace: at least hyenand_scan_backward_workspace_size() bytes, 16-byte
+ * aligned.  gD is reduced in a fixed order: results are deterministic.
+ */
+hyenand_status hyenand_scan_backward(const void* x1, const void* x2, const void* v, const void* log_a, const void* D,
+                                     const int64_t* lengths, const float* states, const void* gy, const float* gh_last,
+                                     void* gx1, void* gx2, void* gv, void* glog_a, void* gD, float* gh0, int64_t B,
+                                     int64_t C, int64_t L, hyenand_dtype dtype, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* Workspace bytes that hyenand_scan_backward takes.  Pure host function. */
+hyenand_status hyenand_scan_backward_workspace_size(int64_t B, int64_t C, int64_t L, hyenand_dtype dtype,
+                                                    size_t* bytes_out);
+
+/*
+ * hyenand_scan_step -- one position of hyenand_scan for every row b of a batch,
+ * on states kept in place: what a decoding loop calls for each token.
+ *
+ * x1, x2, v, log_a, y : [B, C] of dtype; D: [C] of dtype.
+ * state : [num_slots, C] fp32, read and updated.
+ * slots : [B] int64, the state of each row, or NULL for state b of row b
+ *   (num_slots >= B).  A row whose slot lies outside [0, num_slots) is idle:
+ *   it touches no state and its y is 0.  Rows with the same slot are consecutive
+ *   positions of one sequence, in the order of the batch.  States that no row
+ *   names are left as they were.
+ * B <= 65535, B * C < 2^22.  y and state overlap nothing.  No workspace.
+ */
+hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, const void* log_a, const void* D,
+                                 const int64_t* slots, float* state, void* y, int64_t B, int64_t C, int64_t num_slots,
+                                 hyenand_dtype dtype, void* stream);
+
 /* Static text for a status code. */
 const char* hyenand_status_string(hyenand_status status);
 

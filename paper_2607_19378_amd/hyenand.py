@@ -26,7 +26,8 @@ EXPORTED = ("hyenand_fftconv", "hyenand_fftconv_shared_k", "hyenand_fftconv_noal
             "hyenand_kernel_spectrum_size", "hyenand_kernel_spectrum", "hyenand_fftconv_spectrum",
             "hyenand_fftconv_plan_name", "hyenand_fftconv_backward", "hyenand_fftconv_backward_workspace_size",
             "hyenand_fftconv_backward_workspace_min", "hyenand_operator", "hyenand_operator_workspace_size",
-            "hyenand_kernel_synth", "hyenand_modal_filter", "hyenand_status_string", "hyenand_last_error", "hyenand_version")
+            "hyenand_kernel_synth", "hyenand_modal_filter", "hyenand_scan", "hyenand_scan_workspace_size",
+            "hyenand_scan_backward", "hyenand_scan_backward_workspace_size", "hyenand_scan_step", "hyenand_status_string", "hyenand_last_error", "hyenand_version")
 
 _lock = threading.Lock()
 _lib = None
@@ -98,6 +99,15 @@ def lib() -> ctypes.CDLL:
             L.hyenand_modal_filter.argtypes = [vp] * 4 + [ctypes.c_int, vp, ctypes.c_int64, ctypes.c_int64,
                                                        ctypes.c_int, vp]
             L.hyenand_modal_filter.restype = ctypes.c_int
+            i64 = ctypes.c_int64
+            L.hyenand_scan.argtypes = [vp] * 10 + [i64] * 3 + [ctypes.c_int, vp, ctypes.c_size_t, vp]
+            L.hyenand_scan_backward.argtypes = [vp] * 15 + [i64] * 3 + [ctypes.c_int, vp, ctypes.c_size_t, vp]
+            L.hyenand_scan_step.argtypes = [vp] * 8 + [i64] * 3 + [ctypes.c_int, vp]
+            for name in ("hyenand_scan_workspace_size", "hyenand_scan_backward_workspace_size"):
+                getattr(L, name).argtypes = [i64] * 3 + [ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+            for name in ("hyenand_scan", "hyenand_scan_backward", "hyenand_scan_step", "hyenand_scan_workspace_size",
+                         "hyenand_scan_backward_workspace_size"):
+                getattr(L, name).restype = ctypes.c_int
             L.hyenand_fftconv_plan_name.argtypes = [ctypes.c_int, i64p, ctypes.c_int, ctypes.c_int,
                                                     ctypes.c_char_p, ctypes.c_size_t]
             L.hyenand_fftconv_plan_name.restype = ctypes.c_int
@@ -599,3 +609,187 @@ def modal_filter(log_mag, angle, res_re, res_im, L: int, dtype=None, stream=None
     PreparedModal(k, log_mag, angle, res_re, res_im, stream)()
     _keep_for_stream(stream, k)
     return k
+
+
+SCAN_BLOCK = 512  # HYENAND_SCAN_BLOCK: positions between two states that the forward keeps for the backward
+
+
+def _expect(like, shape, dtype, **tensors) -> None:
+    """Every given tensor is contiguous, of this shape and dtype, on `like`'s device."""
+    for name, t in tensors.items():
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
+                              or t.device != like.device):
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {like.device}, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+
+
+def _gpu_dtype(t) -> int:
+    if not t.is_cuda:
+        raise ValueError("all tensors must be on the GPU")
+    return _dtype_code(t.dtype)
+
+
+def _optional(t):
+    return None if t is None else _ptr(t)
+
+
+class _Call:
+    """A marshalled call: enqueues its work again each time it is called, on
+    the same buffers and stream, which it keeps alive."""
+
+    def _prepare(self, fn, args, device, stream, keep) -> None:
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        self._fn, self._args, self._device = fn, args + (ctypes.c_void_p(stream.cuda_stream),), device.index
+        self._current = torch.cuda.current_device
+        self._keep = keep + (stream,)
+
+    def __call__(self) -> None:
+        if self._device == self._current():
+            status = self._fn(*self._args)
+        else:  # launches go to the current device's streams
+            import torch
+            with torch.cuda.device(self._device):
+                status = self._fn(*self._args)
+        if status != OK:
+            _check(status)
+
+
+def _scratch(nbytes: int, workspace, device, stream):
+    """The caller's workspace, or one of nbytes for this call (None if it takes none)."""
+    import torch
+    if workspace is not None:
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    elif nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _keep_for_stream(stream, workspace)
+    return workspace, _optional(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _scan_bytes(fn, shape, dtype) -> int:
+    out = ctypes.c_size_t(0)
+    _check(fn(*[int(n) for n in shape], _dtype_code(dtype), ctypes.byref(out)))
+    return int(out.value)
+
+
+def scan_workspace_size(shape, dtype) -> int:
+    """Workspace bytes of hyenand_scan on [B, C, L] tensors."""
+    return _scan_bytes(lib().hyenand_scan_workspace_size, shape, dtype)
+
+
+def scan_backward_workspace_size(shape, dtype) -> int:
+    return _scan_bytes(lib().hyenand_scan_backward_workspace_size, shape, dtype)
+
+
+def scan_states_shape(shape):
+    """Shape of the states that hyenand_scan keeps for its backward: one before every SCAN_BLOCK-th position."""
+    B, C, L = (int(n) for n in shape)
+    return B, C, -(-L // SCAN_BLOCK)
+
+
+def _scan_inputs(x1, x2, v, log_a, D, lengths):
+    import torch
+    if x1.dim() != 3:
+        raise ValueError(f"x1 must be [B, C, L], got {tuple(x1.shape)}")
+    code, shape = _gpu_dtype(x1), tuple(x1.shape)
+    _expect(x1, shape, x1.dtype, x1=x1, x2=x2, v=v, log_a=log_a)
+    _expect(x1, shape[1:2], x1.dtype, D=D)
+    _expect(x1, shape[:1], torch.int64, lengths=lengths)
+    return code, shape
+
+
+class PreparedScan(_Call):
+    """One hyenand_scan call with its arguments checked and marshalled once
+    (see Prepared).  h0, lengths, h_last and states may be None; h_last may be
+    h0, which then holds the state behind the last position."""
+
+    def __init__(self, y, x1, x2, v, log_a, D, h0=None, lengths=None, h_last=None, states=None, workspace=None,
+                 stream=None):
+        import torch
+        code, shape = _scan_inputs(x1, x2, v, log_a, D, lengths)
+        _expect(x1, shape, x1.dtype, y=y)
+        _expect(x1, shape[:2], torch.float32, h0=h0, h_last=h_last)
+        _expect(x1, scan_states_shape(shape), torch.float32, states=states)
+        ws, ws_ptr, ws_bytes = _scratch(scan_workspace_size(shape, x1.dtype), workspace, x1.device, stream)
+        self._prepare(lib().hyenand_scan,
+                      (_ptr(x1), _ptr(x2), _ptr(v), _ptr(log_a), _ptr(D), _optional(h0), _optional(lengths), _ptr(y),
+                       _optional(h_last), _optional(states)) + shape + (code, ws_ptr, ws_bytes), x1.device, stream,
+                      (y, x1, x2, v, log_a, D, h0, lengths, h_last, states, ws))
+
+
+def scan(x1, x2, v, log_a, D, h0=None, lengths=None, return_last: bool = False, return_states: bool = False,
+         workspace=None, stream=None):
+    """y = x2 * (h + D*u), u = x1*v, h_t = exp(log_a_t) h_{t-1} + u_t on [B, C, L]
+    tensors.  Returns (y, h_last, states), torch-allocated: h_last [B, C] and
+    the states that scan_backward takes where they are asked for, else None."""
+    import torch
+    y = torch.empty_like(x1)
+    last = torch.empty(tuple(x1.shape[:2]), dtype=torch.float32, device=x1.device) if return_last else None
+    states = torch.empty(scan_states_shape(x1.shape), dtype=torch.float32, device=x1.device) if return_states else None
+    PreparedScan(y, x1, x2, v, log_a, D, h0, lengths, last, states, workspace, stream)()
+    _keep_for_stream(stream, y, last, states)
+    return y, last, states
+
+
+class PreparedScanBackward(_Call):
+    """One hyenand_scan_backward call with its arguments checked and
+    marshalled once (see Prepared); lengths, gh_last and gh0 may be None."""
+
+    def __init__(self, gx1, gx2, gv, glog_a, gD, gh0, x1, x2, v, log_a, D, states, gy, lengths=None, gh_last=None,
+                 workspace=None, stream=None):
+        import torch
+        code, shape = _scan_inputs(x1, x2, v, log_a, D, lengths)
+        _expect(x1, shape, x1.dtype, gy=gy, gx1=gx1, gx2=gx2, gv=gv, glog_a=glog_a)
+        _expect(x1, shape[1:2], x1.dtype, gD=gD)
+        _expect(x1, shape[:2], torch.float32, gh_last=gh_last, gh0=gh0)
+        _expect(x1, scan_states_shape(shape), torch.float32, states=states)
+        ws, ws_ptr, ws_bytes = _scratch(scan_backward_workspace_size(shape, x1.dtype), workspace, x1.device, stream)
+        self._prepare(lib().hyenand_scan_backward,
+                      (_ptr(x1), _ptr(x2), _ptr(v), _ptr(log_a), _ptr(D), _optional(lengths), _ptr(states), _ptr(gy),
+                       _optional(gh_last), _ptr(gx1), _ptr(gx2), _ptr(gv), _ptr(glog_a), _ptr(gD), _optional(gh0))
+                      + shape + (code, ws_ptr, ws_bytes), x1.device, stream,
+                      (gx1, gx2, gv, glog_a, gD, gh0, x1, x2, v, log_a, D, states, gy, lengths, gh_last, ws))
+
+
+def scan_backward(x1, x2, v, log_a, D, states, gy, lengths=None, gh_last=None, return_gh0: bool = False,
+                  workspace=None, stream=None):
+    """(gx1, gx2, gv, glog_a, gD), and gh0 with return_gh0, for gy = dLoss/dy
+    (and gh_last = dLoss/dh_last), from the states that scan returned."""
+    import torch
+    gx1, gx2, gv, gla = (torch.empty_like(x1) for _ in range(4))
+    gD = torch.empty_like(D)
+    gh0 = torch.empty(tuple(x1.shape[:2]), dtype=torch.float32, device=x1.device) if return_gh0 else None
+    PreparedScanBackward(gx1, gx2, gv, gla, gD, gh0, x1, x2, v, log_a, D, states, gy, lengths, gh_last, workspace,
+                         stream)()
+    _keep_for_stream(stream, gx1, gx2, gv, gla, gD, gh0)
+    return (gx1, gx2, gv, gla, gD) + ((gh0,) if return_gh0 else ())
+
+
+class PreparedScanStep(_Call):
+    """One hyenand_scan_step call with its arguments checked and marshalled
+    once (see Prepared): y and x1, x2, v, log_a are [B, C], state [slots, C]."""
+
+    def __init__(self, y, x1, x2, v, log_a, D, state, slots=None, stream=None):
+        import torch
+        if x1.dim() != 2 or state.dim() != 2:
+            raise ValueError("x1 must be [B, C] and state [num_slots, C]")
+        code, shape = _gpu_dtype(x1), tuple(x1.shape)
+        _expect(x1, shape, x1.dtype, x1=x1, x2=x2, v=v, log_a=log_a, y=y)
+        _expect(x1, shape[1:], x1.dtype, D=D)
+        _expect(x1, (state.shape[0], shape[1]), torch.float32, state=state)
+        _expect(x1, shape[:1], torch.int64, slots=slots)
+        self._prepare(lib().hyenand_scan_step,
+                      (_ptr(x1), _ptr(x2), _ptr(v), _ptr(log_a), _ptr(D), _optional(slots), _ptr(state), _ptr(y))
+                      + shape + (int(state.shape[0]), code), x1.device, stream, (y, x1, x2, v, log_a, D, state, slots))
+
+
+def scan_step(x1, x2, v, log_a, D, state, slots=None, stream=None):
+    """One position of scan for every row of [B, C] tensors: the rows' states
+    (state[slots[b]], or state[b]) are updated in place; returns y."""
+    import torch
+    y = torch.empty_like(x1)
+    PreparedScanStep(y, x1, x2, v, log_a, D, state, slots, stream)()
+    _keep_for_stream(stream, y)
+    return y
