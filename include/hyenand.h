@@ -520,6 +520,70 @@ hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, 
                                  const int64_t* slots, float* state, void* y, int64_t B, int64_t C, int64_t num_slots,
                                  hyenand_dtype dtype, void* stream);
 
+/*
+ * hyenand_block_norm -- the end of a residual block and the beginning of the next
+ * one on [B, C, P] tensors (P = product of the grid extents), in one pass: the
+ * norm of the gated block output, dropout, the residual scale, the sum with the
+ * stream, and the norm that the next block takes.  The norms run across the C
+ * channels of every sample b and grid point, as in hyenand_operator:
+ *
+ *     t     = Sigmoid(gate) * z
+ *     m     = t / sqrt(mean_c t^2 + eps_post) * w_post[c]         (norm behind the block)
+ *     x_out = x + scale[c] * Drop(m)                              (residual stream)
+ *     n     = x_out / sqrt(mean_c x_out^2 + eps_pre) * w_pre[c]   (norm before the next)
+ *
+ * with Sigmoid(x) = 1 / (1 + exp(-x)).  A point whose root is 0 (a point of zeros
+ * without an eps) has the norm 0.  n is that of x_out before its rounding to dtype.
+ *
+ * x, z, gate, x_out, n : contiguous [B, C, P] of dtype; w_post, scale, w_pre: [C]
+ *   of dtype; all aligned to their element.  gate NULL: no gate.  scale NULL: 1.
+ * First block: z, gate, w_post, scale and x_out NULL, dropout_p 0: n of x alone.
+ * Last block: w_pre and n NULL: x_out alone.
+ * Drop: each point is dropped (0) with the probability dropout_p (0 <= dropout_p
+ *   < 1, taken as the nearest multiple of 2^-16 up to 65535 of them), the others
+ *   are divided by what remains.  The mask is not stored: it is a function of
+ *   rng, a device pointer to two uint64, {seed, offset}, read when the work runs
+ *   (NULL allowed when dropout_p is 0; a captured call draws anew in each replay
+ *   before which they are changed).  The eight points from p = 8 i on of row
+ *   r = b * C + c take the low and high halves, in this order, of the four words
+ *   of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as
+ *   easy as 1, 2, 3", 2011) with the 128-bit counter (r * ceil(P / 8) + i, offset)
+ *   and the key seed, lower words first; a point is dropped where its half is
+ *   below 65536 dropout_p.
+ * B * C < 2^22, P <= 2^40, B * C * P <= 2^46.  No output may overlap an input or
+ * another output.  Compute is fp32; no workspace; validation, stream and error
+ * conventions as for hyenand_fftconv; results are deterministic.
+ */
+hyenand_status hyenand_block_norm(const void* x, const void* z, const void* gate, const void* w_post, const void* scale,
+                                  const void* w_pre, float eps_post, float eps_pre, float dropout_p,
+                                  const uint64_t* rng, void* x_out, void* n, int64_t B, int64_t C, int64_t P,
+                                  hyenand_dtype dtype, void* stream);
+
+/*
+ * hyenand_block_norm_backward -- gradients of a scalar loss through
+ * hyenand_block_norm, given gx_out = dLoss/dx_out (what reaches the stream
+ * directly; NULL: zeros) and gn = dLoss/dn (NULL: n not taken; then w_pre and
+ * gw_pre are NULL), not both NULL.  x_out is the forward's (of a first block, its
+ * x); z, gate, w_post, scale, the eps, dropout_p and rng are the forward's, rng
+ * with the values it had: the mask is drawn again.
+ * Outputs: gx, gz, ggate of dtype [B, C, P] and gw_post, gscale, gw_pre of dtype
+ * [C]; each is given exactly where its input is (gx always).  gx is the gradient
+ * of the forward's x and, with z, of the whole sum: both have the same one.
+ * A point whose norm was 0 by a root of 0 passes no gradient through it.
+ * workspace: at least hyenand_block_norm_backward_workspace_size() bytes, 16-byte
+ * aligned.  The weights' gradients are added up in a fixed order.
+ */
+hyenand_status hyenand_block_norm_backward(const void* x_out, const void* z, const void* gate, const void* w_post,
+                                           const void* scale, const void* w_pre, float eps_post, float eps_pre,
+                                           float dropout_p, const uint64_t* rng, const void* gx_out, const void* gn,
+                                           void* gx, void* gz, void* ggate, void* gw_post, void* gscale, void* gw_pre,
+                                           int64_t B, int64_t C, int64_t P, hyenand_dtype dtype, void* workspace,
+                                           size_t workspace_bytes, void* stream);
+
+/* Workspace bytes that hyenand_block_norm_backward takes.  Pure host function. */
+hyenand_status hyenand_block_norm_backward_workspace_size(int64_t B, int64_t C, int64_t P, hyenand_dtype dtype,
+                                                          size_t* bytes_out);
+
 /* Static text for a status code. */
 const char* hyenand_status_string(hyenand_status status);
 

@@ -1,12 +1,15 @@
 // C-ABI front end of the operators around the long convolution: the gated linear
-// recurrence.  Validation and sizing are pure host code; nothing here touches
+// recurrence, and the norms before and behind a residual block.  Validation and sizing are pure host code; nothing here touches
 // the GPU before every check has passed.
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
 
+#include <cmath>
+
 #include "../../include/hyenand.h"
 #include "kernels.hpp"
+#include "norm.hpp"
 #include "scan.hpp"
 
 namespace hyenand {
@@ -86,6 +89,27 @@ hyenand_status launched(hipError_t e) {
 
 int64_t scan_states_of(int64_t L) { return (L + kScanTile - 1) / kScanTile; }
 static_assert(kScanTile == HYENAND_SCAN_BLOCK, "a state is kept before every tile");
+
+// The arguments that the norms' forward and backward share; x is x_out in the
+// backward.
+hyenand_status check_norm(const void* z, const void* gate, const void* w_post, const void* scale, float eps_post,
+                          float eps_pre, float p, const void* rng, NormArgs* a) {
+  if (!z && (gate || w_post || scale))
+    return fail(HYENAND_ERR_INVALID_ARGUMENT, "gate, w_post and scale belong to a branch z: without it they are NULL");
+  if (z && !w_post) return fail(HYENAND_ERR_INVALID_ARGUMENT, "w_post is NULL");
+  if (!(eps_post >= 0.f) || !(eps_pre >= 0.f) || !std::isfinite(eps_post) || !std::isfinite(eps_pre))
+    return fail(HYENAND_ERR_INVALID_ARGUMENT, "eps_post = %g and eps_pre = %g must be finite and >= 0", (double)eps_post,
+                (double)eps_pre);
+  if (!(p >= 0.f && p < 1.f)) return fail(HYENAND_ERR_INVALID_ARGUMENT, "dropout_p = %g must be in [0, 1)", (double)p);
+  if (p > 0.f && !z) return fail(HYENAND_ERR_INVALID_ARGUMENT, "dropout belongs to a branch z");
+  if (p > 0.f && !rng) return fail(HYENAND_ERR_INVALID_ARGUMENT, "rng is NULL: dropout takes a seed and an offset");
+  const double drop = std::floor((double)p * 65536.0 + 0.5);
+  a->drop = drop > 65535.0 ? 65535u : (uint32_t)drop;
+  a->kept = (float)(65536.0 / (65536.0 - a->drop));
+  a->eps_post = eps_post;
+  a->eps_pre = eps_pre;
+  return HYENAND_OK;
+}
 
 hyenand_status workspace_size(int64_t B, int64_t C, int64_t L, int dtype, bool backward, size_t* bytes_out) {
   if (!bytes_out) return fail(HYENAND_ERR_INVALID_ARGUMENT, "bytes_out is NULL");
@@ -231,6 +255,112 @@ hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, 
   const ScanStepArgs a = {x1, x2, v, log_a, D, slots, state, y, B, num_slots, (int)C, dtype == HYENAND_DTYPE_BF16};
   clear_pending_error();
   return launched(launch_scan_step(a, (hipStream_t)stream));
+}
+
+hyenand_status hyenand_block_norm(const void* x, const void* z, const void* gate, const void* w_post, const void* scale,
+                                  const void* w_pre, float eps_post, float eps_pre, float dropout_p,
+                                  const uint64_t* rng, void* x_out, void* n, int64_t B, int64_t C, int64_t P,
+                                  hyenand_dtype dtype, void* stream) {
+  hyenand_status st = check_shape(B, C, P, "P", dtype);
+  if (st != HYENAND_OK) return st;
+  NormArgs a;
+  memset(&a, 0, sizeof a);
+  st = check_norm(z, gate, w_post, scale, eps_post, eps_pre, dropout_p, rng, &a);
+  if (st != HYENAND_OK) return st;
+  if (!z != !x_out) return fail(HYENAND_ERR_INVALID_ARGUMENT, "z and x_out must both be given or both be NULL");
+  if (!w_pre != !n) return fail(HYENAND_ERR_INVALID_ARGUMENT, "w_pre and n must both be given or both be NULL");
+  if (!z && !n) return fail(HYENAND_ERR_INVALID_ARGUMENT, "neither a branch z nor a norm n is asked for");
+  const size_t es = dtype == HYENAND_DTYPE_BF16 ? 2 : 4, bytes = (size_t)(B * C) * (size_t)P * es, row = (size_t)C * es;
+  const Buffer bufs[] = {{"x", x, bytes, es, false, false},        {"z", z, bytes, es, false, true},
+                         {"gate", gate, bytes, es, false, true},   {"w_post", w_post, row, es, false, true},
+                         {"scale", scale, row, es, false, true},   {"w_pre", w_pre, row, es, false, true},
+                         {"rng", rng, 16, 8, false, true},         {"x_out", x_out, bytes, es, true, true},
+                         {"n", n, bytes, es, true, true}};
+  st = check_buffers(bufs);
+  if (st != HYENAND_OK) return st;
+  a.x = x;
+  a.z = z;
+  a.g = gate;
+  a.w_post = w_post;
+  a.scale = scale;
+  a.w_pre = w_pre;
+  a.rng = rng;
+  a.x_out = x_out;
+  a.n = n;
+  a.B = B;
+  a.C = (int)C;
+  a.P = P;
+  a.bf16 = dtype == HYENAND_DTYPE_BF16;
+  clear_pending_error();
+  return launched(launch_norm(a, (hipStream_t)stream));
+}
+
+hyenand_status hyenand_block_norm_backward_workspace_size(int64_t B, int64_t C, int64_t P, hyenand_dtype dtype,
+                                                          size_t* bytes_out) {
+  if (!bytes_out) return fail(HYENAND_ERR_INVALID_ARGUMENT, "bytes_out is NULL");
+  const hyenand_status st = check_shape(B, C, P, "P", dtype);
+  if (st == HYENAND_OK) *bytes_out = norm_backward_workspace_bytes(B, C, P, dtype == HYENAND_DTYPE_BF16);
+  return st;
+}
+
+hyenand_status hyenand_block_norm_backward(const void* x_out, const void* z, const void* gate, const void* w_post,
+                                           const void* scale, const void* w_pre, float eps_post, float eps_pre,
+                                           float dropout_p, const uint64_t* rng, const void* gx_out, const void* gn,
+                                           void* gx, void* gz, void* ggate, void* gw_post, void* gscale, void* gw_pre,
+                                           int64_t B, int64_t C, int64_t P, hyenand_dtype dtype, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+  hyenand_status st = check_shape(B, C, P, "P", dtype);
+  if (st != HYENAND_OK) return st;
+  NormArgs a;
+  memset(&a, 0, sizeof a);
+  st = check_norm(z, gate, w_post, scale, eps_post, eps_pre, dropout_p, rng, &a);
+  if (st != HYENAND_OK) return st;
+  if (!gx_out && !gn) return fail(HYENAND_ERR_INVALID_ARGUMENT, "neither gx_out nor gn is given");
+  const struct {
+    const void* of;
+    const char* name;
+    const void* grad;
+    const char* grad_name;
+  } pairs[] = {{z, "z", gz, "gz"}, {gate, "gate", ggate, "ggate"}, {w_post, "w_post", gw_post, "gw_post"},
+               {scale, "scale", gscale, "gscale"}, {gn, "gn", w_pre, "w_pre"}, {gn, "gn", gw_pre, "gw_pre"}};
+  for (const auto& q : pairs)
+    if (!q.of != !q.grad)
+      return fail(HYENAND_ERR_INVALID_ARGUMENT, "%s and %s must both be given or both be NULL", q.name, q.grad_name);
+  const size_t es = dtype == HYENAND_DTYPE_BF16 ? 2 : 4, bytes = (size_t)(B * C) * (size_t)P * es, row = (size_t)C * es;
+  const size_t need = norm_backward_workspace_bytes(B, C, P, dtype == HYENAND_DTYPE_BF16);
+  const Buffer bufs[] = {{"x_out", x_out, bytes, es, false, false}, {"z", z, bytes, es, false, true},
+                         {"gate", gate, bytes, es, false, true},    {"w_post", w_post, row, es, false, true},
+                         {"scale", scale, row, es, false, true},    {"w_pre", w_pre, row, es, false, true},
+                         {"rng", rng, 16, 8, false, true},          {"gx_out", gx_out, bytes, es, false, true},
+                         {"gn", gn, bytes, es, false, true},        {"gx", gx, bytes, es, true, false},
+                         {"gz", gz, bytes, es, true, true},         {"ggate", ggate, bytes, es, true, true},
+                         {"gw_post", gw_post, row, es, true, true}, {"gscale", gscale, row, es, true, true},
+                         {"gw_pre", gw_pre, row, es, true, true},   {"workspace", workspace, need, 1, true, true}};
+  st = check_workspace(workspace, workspace_bytes, need);
+  if (st == HYENAND_OK) st = check_buffers(bufs);
+  if (st != HYENAND_OK) return st;
+  a.x = x_out;
+  a.z = z;
+  a.g = gate;
+  a.w_post = w_post;
+  a.scale = scale;
+  a.w_pre = w_pre;
+  a.rng = rng;
+  a.gx_out = gx_out;
+  a.gn = gn;
+  a.gx = gx;
+  a.gz = gz;
+  a.gg = ggate;
+  a.gw_post = gw_post;
+  a.gscale = gscale;
+  a.gw_pre = gw_pre;
+  a.partial = reinterpret_cast<float2*>(workspace);
+  a.B = B;
+  a.C = (int)C;
+  a.P = P;
+  a.bf16 = dtype == HYENAND_DTYPE_BF16;
+  clear_pending_error();
+  return launched(launch_norm_backward(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,34 @@
+// Internal interface of the norms around a block (block_norm.hip).
+#pragma once
+
+#include "kernels.hpp"
+
+namespace hyenand {
+
+// One validated call on [B, C, P] tensors; see include/hyenand.h for the formulas.
+struct NormArgs {
+  const void *x, *z, *g;            // z null: no branch; g null: no gate.  Backward: x is the forward's x_out
+  const void *w_post, *scale, *w_pre;  // scale null: 1
+  const uint64_t* rng;              // {seed, offset} on the device, read where drop > 0
+  void *x_out, *n;                  // n null: no norm behind the sum
+  int64_t B, P;
+  int C;
+  float eps_post, eps_pre;
+  uint32_t drop;                    // a point is dropped where its 16 random bits are below this
+  float kept;                       // what a kept one is multiplied by, 65536 / (65536 - drop)
+  bool bf16;
+  // backward: null where there is none
+  const void *gx_out, *gn;
+  void *gx, *gz, *gg, *gw_post, *gscale, *gw_pre;
+  float2* partial;                  // [groups, C] a workgroup's sums for the weights
+  // set by the launchers
+  int lp;                           // log2 of the lanes over a channel's positions
+  int64_t tiles, row_tiles;         // tiles of positions in all, and of a sample
+  int groups;                       // workgroups of the backward
+};
+
+size_t norm_backward_workspace_bytes(int64_t B, int64_t C, int64_t P, bool bf16);
+hipError_t launch_norm(const NormArgs& a, hipStream_t s);
+hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s);
+
+}  // namespace hyenand

@@ -11,6 +11,7 @@
 
 namespace hyenand {
 
+using namespace rows;
 using namespace scan_dev;
 
 namespace {
@@ -22,15 +23,15 @@ struct FwdTile {
 
 template <typename TS, bool WITH_X2>
 __device__ __forceinline__ void load_fwd(FwdTile<TS>& t, const ScanArgs& a, int64_t off, int n) {
-  t.x1 = load8(reinterpret_cast<const TS*>(a.x1) + off, n);
-  t.v = load8(reinterpret_cast<const TS*>(a.v) + off, n);
-  t.la = load8(reinterpret_cast<const TS*>(a.la) + off, n);
-  if constexpr (WITH_X2) t.x2 = load8(reinterpret_cast<const TS*>(a.x2) + off, n);
+  t.x1 = load(reinterpret_cast<const TS*>(a.x1) + off, n);
+  t.v = load(reinterpret_cast<const TS*>(a.v) + off, n);
+  t.la = load(reinterpret_cast<const TS*>(a.la) + off, n);
+  if constexpr (WITH_X2) t.x2 = load(reinterpret_cast<const TS*>(a.x2) + off, n);
 }
 
 __device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
   if (!a.len) return a.L;
-  const int64_t n = a.len[row / a.C];
+  const int64_t n = a.len[(uint32_t)row / (uint32_t)a.C];
   return n < 0 ? 0 : (n > a.L ? a.L : n);
 }
 
@@ -55,7 +56,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_forward(ScanArgs a)
   __shared__ Span joint[2][W > 1 ? W : 1];
   const Place<G, W> at(a.R);
   const int64_t len = row_length(a, at.row), base = at.row * a.L;
-  const float D = ld1(reinterpret_cast<const TS*>(a.D) + at.row % a.C);
+  const float D = ld1(reinterpret_cast<const TS*>(a.D) + (uint32_t)at.row % (uint32_t)a.C);
   const int64_t seg = blockIdx.y, first = seg * a.seg_tiles;
   const int64_t ntiles = G < 64 ? 1 : (a.L + kScanTile - 1) / kScanTile;
   const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
@@ -63,7 +64,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_forward(ScanArgs a)
   const int64_t in_tile = (int64_t)(at.lane & (G - 1)) * kScanV;
   const int64_t wave = W > 1 ? at.wave : 0;
   auto pos = [&](int64_t tile) { return (tile + wave) * kScanTile + in_tile; };
-  auto count = [&](int64_t tile) { return tile + wave < end ? clamp8(len - pos(tile)) : 0; };
+  auto count = [&](int64_t tile) { return tile + wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
   FwdTile<TS> cur, nxt;
   load_fwd<TS, true>(cur, a, base + pos(first), count(first));
   int buf = 0;
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_forward(ScanArgs a)
       x = advance(s[j], e[j], x, u[j]);
       y[j] = j < n ? get(cur.x2, j) * fmaf(D, u[j], x) : 0.f;
     }
-    if (at.live && tile + wave < end) store8(reinterpret_cast<TS*>(a.y) + base + p, y, clamp8(a.L - p));
+    if (at.live && tile + wave < end) store(reinterpret_cast<TS*>(a.y) + base + p, y, clamp_count<kScanV>(a.L - p));
     if constexpr (G < 64) {
       if (a.h_last && at.live && (at.lane & (G - 1)) == G - 1) a.h_last[at.row] = x;
     } else if constexpr (W == 1) {
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_segment(ScanArgs a)
   const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
   const int64_t in_tile = (int64_t)at.lane * kScanV;
   auto pos = [&](int64_t tile) { return (tile + at.wave) * kScanTile + in_tile; };
-  auto count = [&](int64_t tile) { return tile + at.wave < end ? clamp8(len - pos(tile)) : 0; };
+  auto count = [&](int64_t tile) { return tile + at.wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
   Span sum = {0.f, 0.f};
   FwdTile<TS> cur, nxt;
   load_fwd<TS, false>(cur, a, base + pos(first), count(first));

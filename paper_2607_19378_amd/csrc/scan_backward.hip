@@ -12,6 +12,7 @@
 
 namespace hyenand {
 
+using namespace rows;
 using namespace scan_dev;
 
 namespace {
@@ -23,16 +24,16 @@ struct BwdTile {
 
 template <typename TS>
 __device__ __forceinline__ void load_bwd(BwdTile<TS>& t, const ScanArgs& a, int64_t off, int n) {
-  t.la = load8(reinterpret_cast<const TS*>(a.la) + off, n);
-  t.x1 = load8(reinterpret_cast<const TS*>(a.x1) + off, n);
-  t.v = load8(reinterpret_cast<const TS*>(a.v) + off, n);
-  t.x2 = load8(reinterpret_cast<const TS*>(a.x2) + off, n);
-  t.gy = load8(reinterpret_cast<const TS*>(a.gy) + off, n);
+  t.la = load(reinterpret_cast<const TS*>(a.la) + off, n);
+  t.x1 = load(reinterpret_cast<const TS*>(a.x1) + off, n);
+  t.v = load(reinterpret_cast<const TS*>(a.v) + off, n);
+  t.x2 = load(reinterpret_cast<const TS*>(a.x2) + off, n);
+  t.gy = load(reinterpret_cast<const TS*>(a.gy) + off, n);
 }
 
 __device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
   if (!a.len) return a.L;
-  const int64_t n = a.len[row / a.C];
+  const int64_t n = a.len[(uint32_t)row / (uint32_t)a.C];
   return n < 0 ? 0 : (n > a.L ? a.L : n);
 }
 
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
   __shared__ double sums[W];
   const Place<G, W> at(a.R);
   const int64_t len = row_length(a, at.row), base = at.row * a.L;
-  const float D = ld1(reinterpret_cast<const TS*>(a.D) + at.row % a.C);
+  const float D = ld1(reinterpret_cast<const TS*>(a.D) + (uint32_t)at.row % (uint32_t)a.C);
   const int64_t seg = blockIdx.y, first = seg * a.seg_tiles;
   const int64_t ntiles = G < 64 ? 1 : (a.L + kScanTile - 1) / kScanTile;
   const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
   const int64_t in_tile = (int64_t)(at.lane & (G - 1)) * kScanV;
   const int64_t wave = W > 1 ? at.wave : 0;
   auto pos = [&](int64_t tile) { return (tile + wave) * kScanTile + in_tile; };
-  auto count = [&](int64_t tile) { return tile + wave < end ? clamp8(len - pos(tile)) : 0; };
+  auto count = [&](int64_t tile) { return tile + wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
   auto state = [&](int64_t tile) { return tile + wave < end ? a.states[at.row * a.nst + tile + wave] : 0.f; };
   double gD = 0.0;
   int64_t tile = first + (end - first - 1) / W * W;
@@ -81,7 +82,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
   for (; tile >= first; tile -= W) {
     const int64_t p = pos(tile), off = base + p;
     const int n = count(tile);
-    const int w = at.live && tile + wave < end ? clamp8(a.L - p) : 0;
+    const int w = at.live && tile + wave < end ? clamp_count<kScanV>(a.L - p) : 0;
     if (tile > first) {
       load_bwd(nxt, a, base + pos(tile - W), count(tile - W));
       h_nxt = state(tile - W);
@@ -107,7 +108,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
       dsum = fmaf(gz[j], u[j], dsum);
     }
     gD += dsum;
-    store8(reinterpret_cast<TS*>(a.gx2) + off, out, w);
+    store(reinterpret_cast<TS*>(a.gx2) + off, out, w);
     // c, from behind: the lanes in reverse order
     const Span back = prefix<G>(mirror<G>({sp.s, lane_back(s, e, gz)}), at.lane);
     Span all = {0.f, 0.f};
@@ -128,9 +129,9 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
       g = start ? 0.f : e[j] * g;
       out[j] = j < n && !start ? g * before[j] : 0.f;
     }
-    store8(reinterpret_cast<TS*>(a.gx1) + off, gx1, w);
-    store8(reinterpret_cast<TS*>(a.gv) + off, gv, w);
-    store8(reinterpret_cast<TS*>(a.gla) + off, out, w);
+    store(reinterpret_cast<TS*>(a.gx1) + off, gx1, w);
+    store(reinterpret_cast<TS*>(a.gv) + off, gv, w);
+    store(reinterpret_cast<TS*>(a.gla) + off, out, w);
     if constexpr (G < 64) {
       if (a.gh0 && at.live && (at.lane & (G - 1)) == 0) a.gh0[at.row] = g;
     } else if constexpr (W == 1) {
@@ -168,22 +169,22 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_segment_back(ScanAr
   const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
   const int64_t in_tile = (int64_t)at.lane * kScanV;
   auto pos = [&](int64_t tile) { return (tile + at.wave) * kScanTile + in_tile; };
-  auto count = [&](int64_t tile) { return tile + at.wave < end ? clamp8(len - pos(tile)) : 0; };
-  auto load = [&](BwdTile<TS>& t, int64_t tile) {
+  auto count = [&](int64_t tile) { return tile + at.wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
+  auto fetch = [&](BwdTile<TS>& t, int64_t tile) {
     const int64_t off = base + pos(tile);
     const int n = count(tile);
-    t.la = load8(reinterpret_cast<const TS*>(a.la) + off, n);
-    t.x2 = load8(reinterpret_cast<const TS*>(a.x2) + off, n);
-    t.gy = load8(reinterpret_cast<const TS*>(a.gy) + off, n);
+    t.la = load(reinterpret_cast<const TS*>(a.la) + off, n);
+    t.x2 = load(reinterpret_cast<const TS*>(a.x2) + off, n);
+    t.gy = load(reinterpret_cast<const TS*>(a.gy) + off, n);
   };
   Span sum = {0.f, 0.f};
   int64_t tile = first + (end - first - 1) / W * W;
   BwdTile<TS> cur, nxt;
-  load(cur, tile);
+  fetch(cur, tile);
   int buf = 0;
   for (; tile >= first; tile -= W) {
     const int n = count(tile);
-    if (tile > first) load(nxt, tile - W);
+    if (tile > first) fetch(nxt, tile - W);
     float s[kScanV], e[kScanV], gz[kScanV], total = 0.f;
 #pragma unroll
     for (int j = 0; j < kScanV; ++j) {

@@ -11,6 +11,7 @@
 #pragma once
 
 #include "kernels.hpp"
+#include "row_access.hpp"
 #include "scan.hpp"
 
 namespace hyenand {
@@ -99,61 +100,6 @@ __device__ __forceinline__ Span across_waves(Span mine, Span* at, int wave, int 
   if (wave == 0) return {0.f, 0.f};
   return {read_lane(x.s, wave - 1), read_lane(x.u, wave - 1)};
 }
-
-// Eight consecutive elements as they lie in memory.  A row begins wherever the
-// one before it ends, so that an access is aligned to its element only; gfx950
-// takes 16-byte accesses at such addresses.
-template <typename TS>
-struct Raw {
-  uint32_t w[kScanV * sizeof(TS) / 4];
-};
-
-template <typename TS>
-__device__ __forceinline__ Raw<TS> load8(const TS* p, int n) {
-  Raw<TS> r;
-  if (n >= kScanV) {
-    __builtin_memcpy(&r, p, sizeof r);
-  } else {
-    if constexpr (sizeof(TS) == 2) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        r.w[j] = (2 * j < n ? (uint32_t)p[2 * j] : 0u) | (2 * j + 1 < n ? (uint32_t)p[2 * j + 1] << 16 : 0u);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kScanV; ++j) r.w[j] = j < n ? __float_as_uint(p[j]) : 0u;
-    }
-  }
-  return r;
-}
-
-template <typename TS>
-__device__ __forceinline__ float get(const Raw<TS>& r, int j) {
-  if constexpr (sizeof(TS) == 2)
-    return __uint_as_float((j & 1) ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
-  else
-    return __uint_as_float(r.w[j]);
-}
-
-template <typename TS>
-__device__ __forceinline__ void store8(TS* p, const float (&y)[kScanV], int n) {
-  if (n >= kScanV) {
-    Raw<TS> r;
-    if constexpr (sizeof(TS) == 2) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) r.w[j] = bf16_pack(y[2 * j], y[2 * j + 1]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kScanV; ++j) r.w[j] = __float_as_uint(y[j]);
-    }
-    __builtin_memcpy(p, &r, sizeof r);
-  } else {
-#pragma unroll
-    for (int j = 0; j < kScanV; ++j)
-      if (j < n) st1(p + j, y[j]);
-  }
-}
-
-__device__ __forceinline__ int clamp8(int64_t n) { return n >= kScanV ? kScanV : (n > 0 ? (int)n : 0); }
 
 // log2 a and a of element j; behind the sample's end (j >= n) the state stays as it is
 __device__ __forceinline__ void decay(float la, bool live, float* s, float* e) {

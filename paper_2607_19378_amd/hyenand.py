@@ -27,7 +27,8 @@ EXPORTED = ("hyenand_fftconv", "hyenand_fftconv_shared_k", "hyenand_fftconv_noal
             "hyenand_fftconv_plan_name", "hyenand_fftconv_backward", "hyenand_fftconv_backward_workspace_size",
             "hyenand_fftconv_backward_workspace_min", "hyenand_operator", "hyenand_operator_workspace_size",
             "hyenand_kernel_synth", "hyenand_modal_filter", "hyenand_scan", "hyenand_scan_workspace_size",
-            "hyenand_scan_backward", "hyenand_scan_backward_workspace_size", "hyenand_scan_step", "hyenand_status_string", "hyenand_last_error", "hyenand_version")
+            "hyenand_scan_backward", "hyenand_scan_backward_workspace_size", "hyenand_scan_step", "hyenand_block_norm",
+            "hyenand_block_norm_backward", "hyenand_block_norm_backward_workspace_size", "hyenand_status_string", "hyenand_last_error", "hyenand_version")
 
 _lock = threading.Lock()
 _lib = None
@@ -103,11 +104,16 @@ def lib() -> ctypes.CDLL:
             L.hyenand_scan.argtypes = [vp] * 10 + [i64] * 3 + [ctypes.c_int, vp, ctypes.c_size_t, vp]
             L.hyenand_scan_backward.argtypes = [vp] * 15 + [i64] * 3 + [ctypes.c_int, vp, ctypes.c_size_t, vp]
             L.hyenand_scan_step.argtypes = [vp] * 8 + [i64] * 3 + [ctypes.c_int, vp]
-            for name in ("hyenand_scan_workspace_size", "hyenand_scan_backward_workspace_size"):
+            f32 = ctypes.c_float
+            L.hyenand_block_norm.argtypes = [vp] * 6 + [f32] * 3 + [vp] * 3 + [i64] * 3 + [ctypes.c_int, vp]
+            L.hyenand_block_norm_backward.argtypes = ([vp] * 6 + [f32] * 3 + [vp] * 9 + [i64] * 3
+                                                      + [ctypes.c_int, vp, ctypes.c_size_t, vp])
+            L.hyenand_block_norm.restype = L.hyenand_block_norm_backward.restype = ctypes.c_int
+            for name in ("hyenand_scan_workspace_size", "hyenand_scan_backward_workspace_size",
+                         "hyenand_block_norm_backward_workspace_size"):
                 getattr(L, name).argtypes = [i64] * 3 + [ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
-            for name in ("hyenand_scan", "hyenand_scan_backward", "hyenand_scan_step", "hyenand_scan_workspace_size",
-                         "hyenand_scan_backward_workspace_size"):
                 getattr(L, name).restype = ctypes.c_int
+            L.hyenand_scan.restype = L.hyenand_scan_backward.restype = L.hyenand_scan_step.restype = ctypes.c_int
             L.hyenand_fftconv_plan_name.argtypes = [ctypes.c_int, i64p, ctypes.c_int, ctypes.c_int,
                                                     ctypes.c_char_p, ctypes.c_size_t]
             L.hyenand_fftconv_plan_name.restype = ctypes.c_int
@@ -668,7 +674,7 @@ def _scratch(nbytes: int, workspace, device, stream):
     return workspace, _optional(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
-def _scan_bytes(fn, shape, dtype) -> int:
+def _query(fn, shape, dtype) -> int:
     out = ctypes.c_size_t(0)
     _check(fn(*[int(n) for n in shape], _dtype_code(dtype), ctypes.byref(out)))
     return int(out.value)
@@ -676,11 +682,11 @@ def _scan_bytes(fn, shape, dtype) -> int:
 
 def scan_workspace_size(shape, dtype) -> int:
     """Workspace bytes of hyenand_scan on [B, C, L] tensors."""
-    return _scan_bytes(lib().hyenand_scan_workspace_size, shape, dtype)
+    return _query(lib().hyenand_scan_workspace_size, shape, dtype)
 
 
 def scan_backward_workspace_size(shape, dtype) -> int:
-    return _scan_bytes(lib().hyenand_scan_backward_workspace_size, shape, dtype)
+    return _query(lib().hyenand_scan_backward_workspace_size, shape, dtype)
 
 
 def scan_states_shape(shape):
@@ -793,3 +799,92 @@ def scan_step(x1, x2, v, log_a, D, state, slots=None, stream=None):
     PreparedScanStep(y, x1, x2, v, log_a, D, state, slots, stream)()
     _keep_for_stream(stream, y)
     return y
+
+
+def _points(x):
+    """(B, C, P) of a [B, C, grid...] tensor."""
+    if x.dim() < 2:
+        raise ValueError(f"tensors must be [B, C, grid...], got {tuple(x.shape)}")
+    P = 1
+    for n in x.shape[2:]:
+        P *= int(n)
+    return int(x.shape[0]), int(x.shape[1]), P
+
+
+def block_norm_backward_workspace_size(shape, dtype) -> int:
+    """Workspace bytes of hyenand_block_norm_backward on [B, C, P] tensors."""
+    return _query(lib().hyenand_block_norm_backward_workspace_size, shape, dtype)
+
+
+def _norm_inputs(x, z, gate, w_post, scale, w_pre, rng):
+    import torch
+    code, shape = _gpu_dtype(x), tuple(x.shape)
+    BCP = _points(x)
+    _expect(x, shape, x.dtype, x=x, z=z, gate=gate)
+    _expect(x, shape[1:2], x.dtype, w_post=w_post, scale=scale, w_pre=w_pre)
+    _expect(x, (2,), torch.int64, rng=rng)
+    return code, shape, BCP
+
+
+class PreparedBlockNorm(_Call):
+    """One hyenand_block_norm call with its arguments checked and marshalled
+    once (see Prepared): x_out and n from x, and of z, gate, w_post, scale,
+    w_pre, x_out, n and rng what the call has; the others are None."""
+
+    def __init__(self, x_out, n, x, z=None, gate=None, w_post=None, scale=None, w_pre=None, eps_post: float = 1e-6,
+                 eps_pre: float = 1e-6, dropout_p: float = 0.0, rng=None, stream=None):
+        code, shape, BCP = _norm_inputs(x, z, gate, w_post, scale, w_pre, rng)
+        _expect(x, shape, x.dtype, x_out=x_out, n=n)
+        self._prepare(lib().hyenand_block_norm,
+                      (_ptr(x), _optional(z), _optional(gate), _optional(w_post), _optional(scale), _optional(w_pre),
+                       float(eps_post), float(eps_pre), float(dropout_p), _optional(rng), _optional(x_out), _optional(n))
+                      + BCP + (code,), x.device, stream, (x_out, n, x, z, gate, w_post, scale, w_pre, rng))
+
+
+def block_norm(x, z=None, gate=None, w_post=None, scale=None, w_pre=None, eps_post: float = 1e-6, eps_pre: float = 1e-6,
+               dropout_p: float = 0.0, rng=None, stream=None):
+    """(x_out, n) = (x + scale * drop(RMSNorm(sigmoid(gate) * z) w_post), RMSNorm(x_out) w_pre) on [B, C, grid...]
+    tensors, the norms across the channels, torch-allocated.  Without z: (x, RMSNorm(x) w_pre); without w_pre:
+    (x_out, None).  rng: an int64 GPU tensor (seed, offset), which fixes what dropout drops."""
+    import torch
+    x_out = None if z is None else torch.empty_like(x)
+    n = None if w_pre is None else torch.empty_like(x)
+    PreparedBlockNorm(x_out, n, x, z, gate, w_post, scale, w_pre, eps_post, eps_pre, dropout_p, rng, stream)()
+    _keep_for_stream(stream, x_out, n)
+    return x if z is None else x_out, n
+
+
+class PreparedBlockNormBackward(_Call):
+    """One hyenand_block_norm_backward call with its arguments checked and
+    marshalled once (see Prepared); each gradient but gx is None where its
+    input is (gw_pre, and w_pre, where gn is)."""
+
+    def __init__(self, gx, gz, ggate, gw_post, gscale, gw_pre, x_out, z, gate, w_post, scale, w_pre, gx_out, gn,
+                 eps_post: float = 1e-6, eps_pre: float = 1e-6, dropout_p: float = 0.0, rng=None, workspace=None,
+                 stream=None):
+        code, shape, BCP = _norm_inputs(x_out, z, gate, w_post, scale, w_pre, rng)
+        _expect(x_out, shape, x_out.dtype, gx_out=gx_out, gn=gn, gx=gx, gz=gz, ggate=ggate)
+        _expect(x_out, shape[1:2], x_out.dtype, gw_post=gw_post, gscale=gscale, gw_pre=gw_pre)
+        ws, ws_ptr, ws_bytes = _scratch(block_norm_backward_workspace_size(BCP, x_out.dtype), workspace, x_out.device,
+                                        stream)
+        self._prepare(lib().hyenand_block_norm_backward,
+                      (_ptr(x_out), _optional(z), _optional(gate), _optional(w_post), _optional(scale), _optional(w_pre),
+                       float(eps_post), float(eps_pre), float(dropout_p), _optional(rng), _optional(gx_out), _optional(gn),
+                       _ptr(gx), _optional(gz), _optional(ggate), _optional(gw_post), _optional(gscale), _optional(gw_pre))
+                      + BCP + (code, ws_ptr, ws_bytes), x_out.device, stream,
+                      (gx, gz, ggate, gw_post, gscale, gw_pre, x_out, z, gate, w_post, scale, w_pre, gx_out, gn, rng, ws))
+
+
+def block_norm_backward(x_out, z, gate, w_post, scale, w_pre, gx_out, gn, eps_post: float = 1e-6, eps_pre: float = 1e-6,
+                        dropout_p: float = 0.0, rng=None, workspace=None, stream=None):
+    """(gx, gz, ggate, gw_post, gscale, gw_pre) of block_norm, from its x_out (x where it had no z) and the gradients
+    of x_out and n (either may be None), torch-allocated; None for those of inputs that are None."""
+    import torch
+    if gn is None:
+        w_pre = None
+    like = lambda t: None if t is None else torch.empty_like(t)  # noqa: E731
+    g = (torch.empty_like(x_out),) + tuple(like(t) for t in (z, gate, w_post, scale, w_pre))
+    PreparedBlockNormBackward(*g, x_out, z, gate, w_post, scale, w_pre, gx_out, gn, eps_post, eps_pre, dropout_p, rng,
+                              workspace, stream)()
+    _keep_for_stream(stream, *g)
+    return g

@@ -96,3 +96,53 @@ def keep_factors(B, C, P, p, seed, offset):
             bits[r, g] = [(w[j // 2] >> (16 * (j % 2))) & 0xFFFF for j in range(8)]
     bits = bits.reshape(B, C, groups * 8)[..., :P]
     return (bits >= drop) * (65536.0 / (65536 - drop))
+
+
+def block_norm(x, z=None, gate=None, w_post=None, scale=None, w_pre=None, eps_post=1e-6, eps_pre=1e-6, keep=None):
+    """(x_out, n) of [B, C, P] arrays; keep: the factors of the points."""
+    col = lambda w: 1.0 if w is None else w[None, :, None]  # noqa: E731
+    out = x
+    if z is not None:
+        t = z if gate is None else z / (1 + np.exp(-gate))
+        out = x + col(scale) * (1.0 if keep is None else keep) * (t * inverse_rms(t, eps_post) * col(w_post))
+    return out, None if w_pre is None else out * inverse_rms(out, eps_pre) * col(w_pre)
+
+
+def inverse_rms(t, eps):
+    r = np.sqrt((t * t).mean(1, keepdims=True) + eps)
+    with np.errstate(divide="ignore"):
+        return np.where(r > 0, 1 / r, 0.0)
+
+
+def block_norm_backward(x_out, z=None, gate=None, w_post=None, scale=None, w_pre=None, gx_out=None, gn=None,
+                        eps_post=1e-6, eps_pre=1e-6, keep=None):
+    """Gradients, and for each the magnitude that its roundings are relative to: dict name -> (value, magnitude)."""
+    col = lambda w: 1.0 if w is None else w[None, :, None]  # noqa: E731
+    gx, mag = (np.zeros_like(x_out),) * 2 if gx_out is None else (gx_out, np.abs(gx_out))
+    out = {}
+    if gn is not None:
+        q = inverse_rms(x_out, eps_pre)
+        unit, g = x_out * q, gn * col(w_pre)
+        gx = gx + q * (g - unit * (g * unit).mean(1, keepdims=True))
+        mag = mag + np.abs(q) * (np.abs(g) + np.abs(unit) * np.abs(g * unit).mean(1, keepdims=True))
+        out["gw_pre"] = (gn * unit).sum((0, 2)), np.abs(gn * unit).sum((0, 2))
+    out["gx"] = gx, mag
+    if z is None:
+        return out
+    sig = np.ones_like(z) if gate is None else 1 / (1 + np.exp(-gate))
+    t = sig * z
+    r = inverse_rms(t, eps_post)
+    unit = t * r
+    k = 1.0 if keep is None else keep
+    g, gmag = gx * k * col(scale) * col(w_post), mag * k * np.abs(col(scale) * col(w_post))
+    gt = r * (g - unit * (g * unit).mean(1, keepdims=True))
+    gtmag = r * (gmag + np.abs(unit) * (gmag * np.abs(unit)).mean(1, keepdims=True))
+    out["gz"] = gt * sig, gtmag * sig
+    if gate is not None:
+        rest = 1 / (1 + np.exp(gate))
+        out["ggate"] = gt * t * rest, gtmag * np.abs(t) * rest
+    s, smag = (gx * k * unit), mag * k * np.abs(unit)
+    out["gw_post"] = (s * col(scale)).sum((0, 2)), (smag * np.abs(col(scale))).sum((0, 2))
+    if scale is not None:
+        out["gscale"] = (s * col(w_post)).sum((0, 2)), (smag * np.abs(col(w_post))).sum((0, 2))
+    return out
