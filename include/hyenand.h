@@ -550,8 +550,8 @@ hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, 
  *   easy as 1, 2, 3", 2011) with the 128-bit counter (r * ceil(P / 8) + i, offset)
  *   and the key seed, lower words first; a point is dropped where its half is
  *   below 65536 dropout_p.
- * B * C < 2^22, P <= 2^40, B * C * P <= 2^46.  No output may overlap an input or
- * another output.  Compute is fp32; no workspace; validation, stream and error
+ * B * C < 2^22, B * P <= 2^33.  No output may overlap an input or another
+ * output.  Compute is fp32; no workspace; validation, stream and error
  * conventions as for hyenand_fftconv; results are deterministic.
  */
 hyenand_status hyenand_block_norm(const void* x, const void* z, const void* gate, const void* w_post, const void* scale,

@@ -15,69 +15,78 @@ using namespace norm_dev;
 namespace {
 
 // The tile in registers: K channels a thread.
-template <typename TS, int V, int K>
-__global__ void __launch_bounds__(kMaxNT) norm_forward(NormArgs a) {
-  __shared__ Joint<1> lds;
-  for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-    const Spot<V> at(a, tile);
+template <typename TS, int V, int K, typename Has>
+__global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forward(NormArgs a) {
+  __shared__ Joint<1, V> lds;
+  const Draws draws(a);
+  const int first = threadIdx.x >> a.lp, CL = blockDim.x >> a.lp;
+  float w_post[K], w_pre[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = first + k * CL;
+    w_post[k] = Has::z(a) && c < a.C ? weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) : 0.f;
+    w_pre[k] = Has::n(a) && c < a.C ? weight<TS>(a.w_pre, c) : 0.f;
+  }
+  for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
+    const uint32_t tile = tile_of(a, turn);
+    if (tile >= a.tiles) continue;
+    const Held<TS, V, Has::TAIL> at(a, tile);
     Raw<TS, V> x[K], z[K], g[K];
-    const int64_t base = (at.b * a.C + at.cl) * a.P + at.p, step = (int64_t)at.CL * a.P;
-    auto count = [&](int k) { return at.cl + k * at.CL < a.C ? at.n : 0; };
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (a.z) z[k] = load<TS, V>(reinterpret_cast<const TS*>(a.z) + base + k * step, count(k));
-      if (a.g) g[k] = load<TS, V>(reinterpret_cast<const TS*>(a.g) + base + k * step, count(k));
-      x[k] = load<TS, V>(reinterpret_cast<const TS*>(a.x) + base + k * step, count(k));
+      x[k] = z[k] = g[k] = Raw<TS, V>{};
+      if (first + k * CL < a.C && at.any()) {
+        if (Has::z(a)) z[k] = at.load(a.z, k);
+        if (Has::g(a)) g[k] = at.load(a.g, k);
+        x[k] = at.load(a.x, k);
+      }
     }
     float y[K][V];  // the branch, then the sum
-    float acc[1][V];
-    if (a.z) {
+    float acc[1][V], post[V];
+    if (Has::z(a)) {
 #pragma unroll
       for (int j = 0; j < V; ++j) acc[0][j] = 0.f;
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          float sig = 1.f, rest;
-          if (a.g) gates(get(g[k], j), &sig, &rest);
-          y[k][j] = sig * get(z[k], j);
+          y[k][j] = get(z[k], j);
+          if (Has::g(a)) y[k][j] *= sigmoid_of(gate(get(g[k], j)));
           acc[0][j] = fmaf(y[k][j], y[k][j], acc[0][j]);
         }
-      over_channels(acc, lds, a.lp, at.pg, [&](float (&s)[1]) { s[0] = inverse_rms(s[0], a.C, a.eps_post); });
-      const uint64_t seed = a.drop ? a.rng[0] : 0, offset = a.drop ? a.rng[1] : 0;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int c = at.cl + k * at.CL;
-        const float w = c < a.C ? weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) : 0.f;
-        float f[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = 1.f;
-        if (a.drop) keep_factors<V>(a, seed, offset, at.b * a.C + c, at.p, f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) y[k][j] = fmaf(f[j] * w, y[k][j] * acc[0][j], get(x[k], j));
-        store<TS, V>(reinterpret_cast<TS*>(a.x_out) + base + k * step, y[k], count(k));
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) y[k][j] = get(x[k], j);
+      over_channels(acc, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_post); });
+      read_sums(lds, 0, at.pg, post);
     }
-    if (!a.n) continue;
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[0][j] = 0.f;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+      const int c = first + k * CL;
+      if (Has::z(a)) {
+        uint32_t drawn[4];
+        if (Has::drop(a)) draws.words<V, Has::TAIL>(at.b * a.C + c, at.p, at.shift, drawn);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float w = Has::drop(a) ? draws.factor(drawn, j) * w_post[k] : w_post[k];
+          y[k][j] = fmaf(w, y[k][j] * post[j], get(x[k], j));
+        }
+        if (c < a.C && at.any()) at.store(a.x_out, k, y[k]);
+        __builtin_amdgcn_sched_barrier(0);  // one channel's generator at a time: interleaved, they spill
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[k][j] = get(x[k], j);
+      }
 #pragma unroll
       for (int j = 0; j < V; ++j) acc[0][j] = fmaf(y[k][j], y[k][j], acc[0][j]);
-    over_channels(acc, lds, a.lp, at.pg, [&](float (&s)[1]) { s[0] = inverse_rms(s[0], a.C, a.eps_pre); });
+    }
+    if (!Has::n(a)) continue;
+    over_channels(acc, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_pre); });
+    read_sums(lds, 0, at.pg, post);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = at.cl + k * at.CL;
-      const float w = c < a.C ? weight<TS>(a.w_pre, c) : 0.f;
 #pragma unroll
-      for (int j = 0; j < V; ++j) y[k][j] *= acc[0][j] * w;
-      store<TS, V>(reinterpret_cast<TS*>(a.n) + base + k * step, y[k], count(k));
+      for (int j = 0; j < V; ++j) y[k][j] *= post[j] * w_pre[k];
+      if (first + k * CL < a.C && at.any()) at.store(a.n, k, y[k]);
     }
   }
 }
@@ -85,25 +94,27 @@ __global__ void __launch_bounds__(kMaxNT) norm_forward(NormArgs a) {
 // More channels than registers hold: the tile is read again for each sum.
 template <typename TS, int V>
 __global__ void __launch_bounds__(kMaxNT) norm_forward_reread(NormArgs a) {
-  __shared__ Joint<1> lds;
-  for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+  __shared__ Joint<1, V> lds;
+  for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
+    const uint32_t tile = tile_of(a, turn);
+    if (tile >= a.tiles) continue;
     const Spot<V> at(a, tile);
-    const uint64_t seed = a.drop ? a.rng[0] : 0, offset = a.drop ? a.rng[1] : 0;
+    const int n = clamp_count<V>(a.P - at.p);
+    const Draws draws(a);
     float post[1][V], pre[1][V];
     auto branch = [&](int c, float (&t)[V]) {
       const int64_t o = (at.b * a.C + c) * a.P + at.p;
-      const Raw<TS, V> z = load<TS, V>(reinterpret_cast<const TS*>(a.z) + o, at.n);
+      const Raw<TS, V> z = load<TS, V>(reinterpret_cast<const TS*>(a.z) + o, n);
       Raw<TS, V> g;
-      if (a.g) g = load<TS, V>(reinterpret_cast<const TS*>(a.g) + o, at.n);
+      if (a.g) g = load<TS, V>(reinterpret_cast<const TS*>(a.g) + o, n);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        float sig = 1.f, rest;
-        if (a.g) gates(get(g, j), &sig, &rest);
-        t[j] = sig * get(z, j);
+        t[j] = get(z, j);
+        if (a.g) t[j] *= sigmoid_of(gate(get(g, j)));
       }
     };
     auto sum = [&](int c, float (&y)[V]) {
-      const Raw<TS, V> x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + (at.b * a.C + c) * a.P + at.p, at.n);
+      const Raw<TS, V> x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + (at.b * a.C + c) * a.P + at.p, n);
       if (!a.z) {
 #pragma unroll
         for (int j = 0; j < V; ++j) y[j] = get(x, j);
@@ -111,12 +122,10 @@ __global__ void __launch_bounds__(kMaxNT) norm_forward_reread(NormArgs a) {
       }
       branch(c, y);
       const float w = weight<TS>(a.w_post, c) * weight<TS>(a.scale, c);
-      float f[V];
+      uint32_t drawn[4];
+      if (a.drop) draws.words<V, false>(at.b * a.C + c, at.p, 0, drawn);
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = 1.f;
-      if (a.drop) keep_factors<V>(a, seed, offset, at.b * a.C + c, at.p, f);
-#pragma unroll
-      for (int j = 0; j < V; ++j) y[j] = fmaf(f[j] * w, y[j] * post[0][j], get(x, j));
+      for (int j = 0; j < V; ++j) y[j] = fmaf(a.drop ? draws.factor(drawn, j) * w : w, y[j] * post[0][j], get(x, j));
     };
 #pragma unroll
     for (int j = 0; j < V; ++j) post[0][j] = pre[0][j] = 0.f;
@@ -127,84 +136,125 @@ __global__ void __launch_bounds__(kMaxNT) norm_forward_reread(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) post[0][j] = fmaf(t[j], t[j], post[0][j]);
       }
-      over_channels(post, lds, a.lp, at.pg, [&](float (&s)[1]) { s[0] = inverse_rms(s[0], a.C, a.eps_post); });
+      over_channels(post, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_post); });
+      read_sums(lds, 0, at.pg, post[0]);
     }
     for (int c = at.cl; c < a.C; c += at.CL) {
       float y[V];
       sum(c, y);
-      if (a.z) store<TS, V>(reinterpret_cast<TS*>(a.x_out) + (at.b * a.C + c) * a.P + at.p, y, at.n);
+      if (a.z) store<TS, V>(reinterpret_cast<TS*>(a.x_out) + (at.b * a.C + c) * a.P + at.p, y, n);
 #pragma unroll
       for (int j = 0; j < V; ++j) pre[0][j] = fmaf(y[j], y[j], pre[0][j]);
     }
     if (!a.n) continue;
-    over_channels(pre, lds, a.lp, at.pg, [&](float (&s)[1]) { s[0] = inverse_rms(s[0], a.C, a.eps_pre); });
+    over_channels(pre, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_pre); });
+    read_sums(lds, 0, at.pg, pre[0]);
     for (int c = at.cl; c < a.C; c += at.CL) {
       float y[V];
       sum(c, y);
       const float w = weight<TS>(a.w_pre, c);
 #pragma unroll
       for (int j = 0; j < V; ++j) y[j] *= pre[0][j] * w;
-      store<TS, V>(reinterpret_cast<TS*>(a.n) + (at.b * a.C + c) * a.P + at.p, y, at.n);
+      store<TS, V>(reinterpret_cast<TS*>(a.n) + (at.b * a.C + c) * a.P + at.p, y, n);
     }
   }
 }
 
-constexpr int64_t kMaxGrid = int64_t(1) << 20;  // workgroups of a launch (fewer than 2^32 work-items)
+constexpr uint32_t kMaxGrid = 1u << 20;  // workgroups of a launch (fewer than 2^32 work-items)
+
+template <typename TS, typename Has>
+hipError_t forward_held(const NormArgs& a, const NormShape& s, hipStream_t st) {
+  const dim3 grid((unsigned)(a.turns < kMaxGrid ? a.turns : kMaxGrid)), block((unsigned)s.NT);
+  constexpr int V = 16 / sizeof(TS);
+#define HY_CASE(v, k) \
+  if (s.V == v && s.K == k) hipLaunchKernelGGL((norm_forward<TS, v, k, Has>), grid, block, 0, st, a);
+  if constexpr (!Has::TAIL) {
+    HY_CASE(1, 1) HY_CASE(1, 4) HY_CASE(1, 8)
+  }
+  HY_CASE(V, 1) HY_CASE(V, 2) HY_CASE(V, 4) HY_CASE(V, 8)
+#undef HY_CASE
+  return hipGetLastError();
+}
+
+template <typename TS, bool TAIL>
+hipError_t forward_parts(const NormArgs& a, const NormShape& s, hipStream_t st) {
+  if (!a.z || !a.n) return forward_held<TS, Parts<false, false, false, TAIL>>(a, s, st);
+  if (a.drop)
+    return a.g ? forward_held<TS, Parts<true, true, true, TAIL>>(a, s, st)
+               : forward_held<TS, Parts<true, false, true, TAIL>>(a, s, st);
+  return a.g ? forward_held<TS, Parts<true, true, false, TAIL>>(a, s, st)
+             : forward_held<TS, Parts<true, false, false, TAIL>>(a, s, st);
+}
 
 template <typename TS>
 hipError_t forward(const NormArgs& a, const NormShape& s, hipStream_t st) {
-  const dim3 grid((unsigned)(a.tiles < kMaxGrid ? a.tiles : kMaxGrid)), block((unsigned)s.NT);
-#define HY_CASE(v, k) \
-  if (s.V == v && s.K == k) hipLaunchKernelGGL((norm_forward<TS, v, k>), grid, block, 0, st, a);
-  HY_CASE(1, 1) HY_CASE(1, 4) HY_CASE(1, 16) HY_CASE(8, 1) HY_CASE(8, 2) HY_CASE(8, 4)
-#undef HY_CASE
-  if (s.K == 0) {
-    if (s.V == 1) hipLaunchKernelGGL((norm_forward_reread<TS, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((norm_forward_reread<TS, 8>), grid, block, 0, st, a);
-  }
+  if (s.K > 0) return a.P % s.V == 0 ? forward_parts<TS, false>(a, s, st) : forward_parts<TS, true>(a, s, st);
+  const dim3 grid((unsigned)(a.turns < kMaxGrid ? a.turns : kMaxGrid)), block((unsigned)s.NT);
+  constexpr int V = 16 / sizeof(TS);
+  if (s.V == 1) hipLaunchKernelGGL((norm_forward_reread<TS, 1>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((norm_forward_reread<TS, V>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-NormShape norm_shape(int64_t C, int64_t P, bool bf16, bool backward) {
+// A row's accesses are as wide as 8 lanes make them (128 bytes), since narrower
+// ones cost most (8 x 256 x 64 x 64 fp32 forward: 40 us at 128 bytes, 45, 48 and 61 us
+// at 64, 32 and 16; backward of 2 x 512 x 8192 bf16: 50 us at 64 bytes, 73 and 85 us
+// at 32 and 16), as far as the channels then fit.  The forward takes four channels a
+// thread in 512 threads where two would need 1024 (2 x 512 x 8192 bf16: 21 against
+// 24 us, two workgroups a CU), unless that leaves CUs without a tile; eight only
+// where four would halve the width to 16 bytes (2 x 2048 x 2048 bf16: 30 against
+// 34 us; 2 x 512 x 8192: 27 against 21 us for 128 bytes in place of 64).  The backward
+// takes as few channels a thread as fit (2 x 512 x 8192 bf16: 50 us with two, 56 us
+// with four).
+NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) {
   NormShape s;
-  s.V = P == 1 ? 1 : 8;
-  s.lp = 0;
+  const int V = bf16 ? 8 : 4;
+  s.V = P < V ? 1 : V;
+  auto threads = [&](int K, int lp) { return (((C + K - 1) / K << lp) + 63) / 64 * 64; };
+  auto take = [&](int K, int lp, int most) {
+    if (threads(K, lp) > most) return false;
+    s.K = K;
+    s.lp = lp;
+    s.NT = (int)threads(K, lp);
+    return true;
+  };
   const int64_t groups = (P + s.V - 1) / s.V;
-  // a cache line of a row (128 bytes) where the row is as long
-  const int most = s.V == 1 ? 0 : (bf16 ? 3 : 2);
-  while (s.lp < most && (int64_t(1) << s.lp) < groups) ++s.lp;
-  const int ks_many[] = {1, 4, 16}, ks_fwd[] = {1, 2, 4}, ks_bwd[] = {1, 2, bf16 ? 4 : 2};
-  const int(&ks)[3] = s.V == 1 ? ks_many : (backward ? ks_bwd : ks_fwd);
-  // channels a thread: the fewest of which 1024 threads hold all; fewer points
-  // a tile where the most are not enough
-  for (;; --s.lp) {
-    for (int k : ks) {
-      const int64_t nt = ((C + k - 1) / k << s.lp) + 63;
-      if (nt / 64 * 64 <= kMaxNT) {
-        s.K = k;
-        s.NT = (int)(nt / 64 * 64);
-        return s;
+  int lp = 0;
+  while (lp < 3 && (int64_t(1) << lp) < groups) ++lp;
+  // 32-bit offsets in a sample's tensors
+  if (C * P <= (int64_t(1) << 32) / (bf16 ? 2 : 4) - 4096) {
+    for (; lp >= 0; --lp) {
+      if (s.V == 1) {
+        if (take(1, lp, kMaxNT) || take(4, lp, kMaxNT) || take(8, lp, kMaxNT)) return s;
+        continue;
       }
+      const bool many = (groups >> lp) * B >= 512;
+      if (!backward && many && (take(1, lp, 512) || take(2, lp, 512) || take(4, lp, 512))) return s;
+      if (take(1, lp, kMaxNT) || take(2, lp, kMaxNT) || take(4, lp, norm_threads(4))) return s;
+      if (!backward && lp == 1 && take(8, lp, norm_threads(8))) return s;
     }
-    if (s.lp == 0) break;
   }
+  s.lp = 0;
   s.K = 0;
   s.NT = kMaxNT;
   return s;
 }
 
 void norm_tiles(NormArgs& a, const NormShape& s) {
+  const int64_t points = (int64_t)s.V << s.lp, row_tiles = (a.P + points - 1) / points;
   a.lp = s.lp;
-  const int64_t points = (int64_t)s.V << s.lp;
-  a.row_tiles = (a.P + points - 1) / points;
-  a.tiles = a.row_tiles * a.B;
+  a.row_tiles = (uint32_t)row_tiles;
+  a.tiles = (uint32_t)(row_tiles * a.B);  // fewer than 2^31 + 2^22: kMaxNormPoints points, of which a tile has 4 or a row's
+  a.log_run = 4 - s.lp;  // 16 lanes' points: two cache lines
+  const uint32_t round = 8u << a.log_run;
+  a.turns = (a.tiles + round - 1) / round * round;
 }
 
 hipError_t launch_norm(const NormArgs& args, hipStream_t st) {
   NormArgs a = args;
-  const NormShape s = norm_shape(a.C, a.P, a.bf16, false);
+  const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, false);
   norm_tiles(a, s);
   return a.bf16 ? forward<uint16_t>(a, s, st) : forward<float>(a, s, st);
 }

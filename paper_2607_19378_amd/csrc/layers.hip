@@ -87,6 +87,15 @@ hyenand_status launched(hipError_t e) {
   return e == hipSuccess ? HYENAND_OK : fail(HYENAND_ERR_HIP, "HIP error %d: %s", (int)e, hipGetErrorString(e));
 }
 
+hyenand_status check_norm_shape(int64_t B, int64_t C, int64_t P, int dtype) {
+  const hyenand_status st = check_shape(B, C, P, "P", dtype);
+  if (st != HYENAND_OK) return st;
+  if (P > kMaxNormPoints / B)
+    return fail(HYENAND_ERR_UNSUPPORTED, "B * P = %lld x %lld points exceed the %lld one call takes", (long long)B,
+                (long long)P, (long long)kMaxNormPoints);
+  return HYENAND_OK;
+}
+
 int64_t scan_states_of(int64_t L) { return (L + kScanTile - 1) / kScanTile; }
 static_assert(kScanTile == HYENAND_SCAN_BLOCK, "a state is kept before every tile");
 
@@ -261,7 +270,7 @@ hyenand_status hyenand_block_norm(const void* x, const void* z, const void* gate
                                   const void* w_pre, float eps_post, float eps_pre, float dropout_p,
                                   const uint64_t* rng, void* x_out, void* n, int64_t B, int64_t C, int64_t P,
                                   hyenand_dtype dtype, void* stream) {
-  hyenand_status st = check_shape(B, C, P, "P", dtype);
+  hyenand_status st = check_norm_shape(B, C, P, dtype);
   if (st != HYENAND_OK) return st;
   NormArgs a;
   memset(&a, 0, sizeof a);
@@ -298,7 +307,7 @@ hyenand_status hyenand_block_norm(const void* x, const void* z, const void* gate
 hyenand_status hyenand_block_norm_backward_workspace_size(int64_t B, int64_t C, int64_t P, hyenand_dtype dtype,
                                                           size_t* bytes_out) {
   if (!bytes_out) return fail(HYENAND_ERR_INVALID_ARGUMENT, "bytes_out is NULL");
-  const hyenand_status st = check_shape(B, C, P, "P", dtype);
+  const hyenand_status st = check_norm_shape(B, C, P, dtype);
   if (st == HYENAND_OK) *bytes_out = norm_backward_workspace_bytes(B, C, P, dtype == HYENAND_DTYPE_BF16);
   return st;
 }
@@ -309,7 +318,7 @@ hyenand_status hyenand_block_norm_backward(const void* x_out, const void* z, con
                                            void* gx, void* gz, void* ggate, void* gw_post, void* gscale, void* gw_pre,
                                            int64_t B, int64_t C, int64_t P, hyenand_dtype dtype, void* workspace,
                                            size_t workspace_bytes, void* stream) {
-  hyenand_status st = check_shape(B, C, P, "P", dtype);
+  hyenand_status st = check_norm_shape(B, C, P, dtype);
   if (st != HYENAND_OK) return st;
   NormArgs a;
   memset(&a, 0, sizeof a);

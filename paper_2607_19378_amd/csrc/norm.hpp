@@ -23,9 +23,13 @@ struct NormArgs {
   float2* partial;                  // [groups, C] a workgroup's sums for the weights
   // set by the launchers
   int lp;                           // log2 of the lanes over a channel's positions
-  int64_t tiles, row_tiles;         // tiles of positions in all, and of a sample
+  uint32_t tiles, row_tiles;        // tiles of points in all, and of a sample
+  uint32_t log_run;                 // log2 of the consecutive tiles of an XCD's turn
+  uint32_t turns;                   // tiles, and the turns that fall behind the last one
   int groups;                       // workgroups of the backward
 };
+
+constexpr int64_t kMaxNormPoints = int64_t(1) << 33;  // B * P: tiles are counted in 32 bits
 
 size_t norm_backward_workspace_bytes(int64_t B, int64_t C, int64_t P, bool bf16);
 hipError_t launch_norm(const NormArgs& a, hipStream_t s);

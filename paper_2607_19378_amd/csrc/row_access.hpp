@@ -6,7 +6,7 @@
 namespace hyenand {
 namespace rows {
 
-// V = 8 or 1 consecutive elements as they lie in memory.  A row begins wherever
+// V = 8, 4 or 1 consecutive elements as they lie in memory.  A row begins wherever
 // the one before it ends, so that an access is aligned to its element only;
 // gfx950 takes 16-byte accesses at such addresses.
 template <typename TS, int V = 8>
@@ -61,6 +61,21 @@ __device__ __forceinline__ void store(TS* p, const float (&y)[V], int n) {
     for (int j = 0; j < V; ++j)
       if (j < n) st1(p + j, y[j]);
   }
+}
+
+// V elements at a byte offset from an address that is the same for all lanes
+template <typename TS, int V>
+__device__ __forceinline__ Raw<TS, V> load_at(const void* base, uint32_t off) {
+  Raw<TS, V> r;
+  if constexpr (V == 1)
+    r.w[0] = __float_as_uint(ld1(reinterpret_cast<const TS*>(reinterpret_cast<const char*>(base) + off)));
+  else
+    __builtin_memcpy(&r, reinterpret_cast<const char*>(base) + off, sizeof r);
+  return r;
+}
+template <typename TS, int V>
+__device__ __forceinline__ void store_at(void* base, uint32_t off, const float (&y)[V]) {
+  store<TS, V>(reinterpret_cast<TS*>(reinterpret_cast<char*>(base) + off), y, V);
 }
 
 template <int V>
