@@ -8,6 +8,8 @@ call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import math
 import os
 import threading
 from typing import Optional, Sequence
@@ -622,11 +624,13 @@ SCAN_BLOCK = 512  # HYENAND_SCAN_BLOCK: positions between two states that the fo
 
 def _expect(like, shape, dtype, **tensors) -> None:
     """Every given tensor is contiguous, of this shape and dtype, on `like`'s device."""
-    for name, t in tensors.items():
-        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
-                              or t.device != like.device):
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {like.device}, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+    device = like.get_device()
+    for t in tensors.values():
+        if t is None or (t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == device):
+            continue
+        name = next(n for n, u in tensors.items() if u is t)
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {like.device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
 
 
 def _gpu_dtype(t) -> int:
@@ -635,8 +639,8 @@ def _gpu_dtype(t) -> int:
     return _dtype_code(t.dtype)
 
 
-def _optional(t):
-    return None if t is None else _ptr(t)
+def _pointers(*tensors):
+    return tuple([None if t is None else t.data_ptr() for t in tensors])
 
 
 class _Call:
@@ -647,9 +651,10 @@ class _Call:
         import torch
         if stream is None:
             stream = torch.cuda.current_stream(device)
-        self._fn, self._args, self._device = fn, args + (ctypes.c_void_p(stream.cuda_stream),), device.index
+        self._fn, self._device = fn, device.index
+        self._args = args + (stream.cuda_stream,)
         self._current = torch.cuda.current_device
-        self._keep = keep + (stream,)
+        self._keep = (keep, stream)
 
     def __call__(self) -> None:
         if self._device == self._current():
@@ -671,22 +676,25 @@ def _scratch(nbytes: int, workspace, device, stream):
     elif nbytes:
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         _keep_for_stream(stream, workspace)
-    return workspace, _optional(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is None:
+        return None, None, 0
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _query(fn, shape, dtype) -> int:
+@functools.lru_cache(maxsize=1024)
+def _query(name: str, shape, code: int) -> int:
     out = ctypes.c_size_t(0)
-    _check(fn(*[int(n) for n in shape], _dtype_code(dtype), ctypes.byref(out)))
+    _check(getattr(lib(), name)(*[int(n) for n in shape], code, ctypes.byref(out)))
     return int(out.value)
 
 
 def scan_workspace_size(shape, dtype) -> int:
     """Workspace bytes of hyenand_scan on [B, C, L] tensors."""
-    return _query(lib().hyenand_scan_workspace_size, shape, dtype)
+    return _query("hyenand_scan_workspace_size", tuple(shape), _dtype_code(dtype))
 
 
 def scan_backward_workspace_size(shape, dtype) -> int:
-    return _query(lib().hyenand_scan_backward_workspace_size, shape, dtype)
+    return _query("hyenand_scan_backward_workspace_size", tuple(shape), _dtype_code(dtype))
 
 
 def scan_states_shape(shape):
@@ -720,8 +728,8 @@ class PreparedScan(_Call):
         _expect(x1, scan_states_shape(shape), torch.float32, states=states)
         ws, ws_ptr, ws_bytes = _scratch(scan_workspace_size(shape, x1.dtype), workspace, x1.device, stream)
         self._prepare(lib().hyenand_scan,
-                      (_ptr(x1), _ptr(x2), _ptr(v), _ptr(log_a), _ptr(D), _optional(h0), _optional(lengths), _ptr(y),
-                       _optional(h_last), _optional(states)) + shape + (code, ws_ptr, ws_bytes), x1.device, stream,
+                      _pointers(x1, x2, v, log_a, D, h0, lengths, y, h_last, states) + shape + (code, ws_ptr, ws_bytes),
+                      x1.device, stream,
                       (y, x1, x2, v, log_a, D, h0, lengths, h_last, states, ws))
 
 
@@ -753,8 +761,7 @@ class PreparedScanBackward(_Call):
         _expect(x1, scan_states_shape(shape), torch.float32, states=states)
         ws, ws_ptr, ws_bytes = _scratch(scan_backward_workspace_size(shape, x1.dtype), workspace, x1.device, stream)
         self._prepare(lib().hyenand_scan_backward,
-                      (_ptr(x1), _ptr(x2), _ptr(v), _ptr(log_a), _ptr(D), _optional(lengths), _ptr(states), _ptr(gy),
-                       _optional(gh_last), _ptr(gx1), _ptr(gx2), _ptr(gv), _ptr(glog_a), _ptr(gD), _optional(gh0))
+                      _pointers(x1, x2, v, log_a, D, lengths, states, gy, gh_last, gx1, gx2, gv, glog_a, gD, gh0)
                       + shape + (code, ws_ptr, ws_bytes), x1.device, stream,
                       (gx1, gx2, gv, glog_a, gD, gh0, x1, x2, v, log_a, D, states, gy, lengths, gh_last, ws))
 
@@ -787,8 +794,7 @@ class PreparedScanStep(_Call):
         _expect(x1, (state.shape[0], shape[1]), torch.float32, state=state)
         _expect(x1, shape[:1], torch.int64, slots=slots)
         self._prepare(lib().hyenand_scan_step,
-                      (_ptr(x1), _ptr(x2), _ptr(v), _ptr(log_a), _ptr(D), _optional(slots), _ptr(state), _ptr(y))
-                      + shape + (int(state.shape[0]), code), x1.device, stream, (y, x1, x2, v, log_a, D, state, slots))
+                      _pointers(x1, x2, v, log_a, D, slots, state, y) + shape + (int(state.shape[0]), code), x1.device, stream, (y, x1, x2, v, log_a, D, state, slots))
 
 
 def scan_step(x1, x2, v, log_a, D, state, slots=None, stream=None):
@@ -801,25 +807,22 @@ def scan_step(x1, x2, v, log_a, D, state, slots=None, stream=None):
     return y
 
 
-def _points(x):
+def _points(shape):
     """(B, C, P) of a [B, C, grid...] tensor."""
-    if x.dim() < 2:
-        raise ValueError(f"tensors must be [B, C, grid...], got {tuple(x.shape)}")
-    P = 1
-    for n in x.shape[2:]:
-        P *= int(n)
-    return int(x.shape[0]), int(x.shape[1]), P
+    if len(shape) < 2:
+        raise ValueError(f"tensors must be [B, C, grid...], got {shape}")
+    return shape[0], shape[1], math.prod(shape[2:])
 
 
 def block_norm_backward_workspace_size(shape, dtype) -> int:
     """Workspace bytes of hyenand_block_norm_backward on [B, C, P] tensors."""
-    return _query(lib().hyenand_block_norm_backward_workspace_size, shape, dtype)
+    return _query("hyenand_block_norm_backward_workspace_size", tuple(shape), _dtype_code(dtype))
 
 
 def _norm_inputs(x, z, gate, w_post, scale, w_pre, rng):
     import torch
     code, shape = _gpu_dtype(x), tuple(x.shape)
-    BCP = _points(x)
+    BCP = _points(shape)
     _expect(x, shape, x.dtype, x=x, z=z, gate=gate)
     _expect(x, shape[1:2], x.dtype, w_post=w_post, scale=scale, w_pre=w_pre)
     _expect(x, (2,), torch.int64, rng=rng)
@@ -836,9 +839,8 @@ class PreparedBlockNorm(_Call):
         code, shape, BCP = _norm_inputs(x, z, gate, w_post, scale, w_pre, rng)
         _expect(x, shape, x.dtype, x_out=x_out, n=n)
         self._prepare(lib().hyenand_block_norm,
-                      (_ptr(x), _optional(z), _optional(gate), _optional(w_post), _optional(scale), _optional(w_pre),
-                       float(eps_post), float(eps_pre), float(dropout_p), _optional(rng), _optional(x_out), _optional(n))
-                      + BCP + (code,), x.device, stream, (x_out, n, x, z, gate, w_post, scale, w_pre, rng))
+                      _pointers(x, z, gate, w_post, scale, w_pre) + (eps_post, eps_pre, dropout_p)
+                      + _pointers(rng, x_out, n) + BCP + (code,), x.device, stream, (x_out, n, x, z, gate, w_post, scale, w_pre, rng))
 
 
 def block_norm(x, z=None, gate=None, w_post=None, scale=None, w_pre=None, eps_post: float = 1e-6, eps_pre: float = 1e-6,
@@ -868,10 +870,8 @@ class PreparedBlockNormBackward(_Call):
         ws, ws_ptr, ws_bytes = _scratch(block_norm_backward_workspace_size(BCP, x_out.dtype), workspace, x_out.device,
                                         stream)
         self._prepare(lib().hyenand_block_norm_backward,
-                      (_ptr(x_out), _optional(z), _optional(gate), _optional(w_post), _optional(scale), _optional(w_pre),
-                       float(eps_post), float(eps_pre), float(dropout_p), _optional(rng), _optional(gx_out), _optional(gn),
-                       _ptr(gx), _optional(gz), _optional(ggate), _optional(gw_post), _optional(gscale), _optional(gw_pre))
-                      + BCP + (code, ws_ptr, ws_bytes), x_out.device, stream,
+                      _pointers(x_out, z, gate, w_post, scale, w_pre) + (eps_post, eps_pre, dropout_p)
+                      + _pointers(rng, gx_out, gn, gx, gz, ggate, gw_post, gscale, gw_pre) + BCP + (code, ws_ptr, ws_bytes), x_out.device, stream,
                       (gx, gz, ggate, gw_post, gscale, gw_pre, x_out, z, gate, w_post, scale, w_pre, gx_out, gn, rng, ws))
 
 
