@@ -307,6 +307,7 @@ __global__ void __launch_bounds__(1024) norm_weights(NormArgs a) {
   const int c = blockIdx.x * 32 + lane;
   double x = 0.0, y = 0.0;
   if (c < a.C)
+#pragma unroll 8
     for (int i = part; i < a.groups; i += 32) {
       const float2 w = a.partial[(int64_t)i * a.C + c];
       x += w.x;

@@ -13,6 +13,7 @@
 namespace hyenand {
 namespace norm_dev {
 
+using rows::keep_packed;
 using rows::Raw;
 
 constexpr int kMaxNT = 1024;
@@ -268,19 +269,6 @@ __device__ __forceinline__ void read_sums(const Joint<M, V>& lds, int m, int pg,
   for (int j = 0; j < N; ++j) x[j] = lds.all[m][pg * V + from + j];
 }
 __device__ __forceinline__ void next_channel() { asm volatile("" ::: "memory"); }
-
-// Values that come from x are computed from it again after this, instead of being
-// kept beside it: a row of bf16 takes half the registers of what it unpacks to.
-template <typename TS, int V>
-__device__ __forceinline__ void keep_packed(Raw<TS, V>& x) {
-#pragma unroll
-  for (uint32_t& w : x.w) asm volatile("" : "+v"(w));
-}
-template <int V>
-__device__ __forceinline__ void keep_packed(float (&x)[V]) {
-#pragma unroll
-  for (float& w : x) asm volatile("" : "+v"(w));
-}
 
 // What a call has: known beforehand for a block with its branch and both norms
 // (KNOWN), looked up for the others.  TAIL: see Held.

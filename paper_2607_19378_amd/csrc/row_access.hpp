@@ -78,6 +78,14 @@ __device__ __forceinline__ void store_at(void* base, uint32_t off, const float (
   store<TS, V>(reinterpret_cast<TS*>(reinterpret_cast<char*>(base) + off), y, V);
 }
 
+// Values that come from x are computed from it again after this, instead of being
+// kept beside it: a row of bf16 takes half the registers of what it unpacks to.
+template <typename TS, int V>
+__device__ __forceinline__ void keep_packed(Raw<TS, V>& x) {
+#pragma unroll
+  for (uint32_t& w : x.w) asm volatile("" : "+v"(w));
+}
+
 template <int V>
 __device__ __forceinline__ int clamp_count(int64_t n) {
   return n >= V ? V : (n > 0 ? (int)n : 0);

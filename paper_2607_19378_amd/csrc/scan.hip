@@ -21,72 +21,85 @@ struct FwdTile {
   Raw<TS> x1, v, la, x2;
 };
 
-template <typename TS, bool WITH_X2>
+template <typename TS>
 __device__ __forceinline__ void load_fwd(FwdTile<TS>& t, const ScanArgs& a, int64_t off, int n) {
   t.x1 = load(reinterpret_cast<const TS*>(a.x1) + off, n);
   t.v = load(reinterpret_cast<const TS*>(a.v) + off, n);
   t.la = load(reinterpret_cast<const TS*>(a.la) + off, n);
-  if constexpr (WITH_X2) t.x2 = load(reinterpret_cast<const TS*>(a.x2) + off, n);
+  t.x2 = load(reinterpret_cast<const TS*>(a.x2) + off, n);
 }
 
-__device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
-  if (!a.len) return a.L;
-  const int64_t n = a.len[(uint32_t)row / (uint32_t)a.C];
-  return n < 0 ? 0 : (n > a.L ? a.L : n);
-}
-
-// The span of a lane's eight positions.
 template <typename TS>
-__device__ __forceinline__ Span lane_span(const FwdTile<TS>& t, int n, float (&s)[kScanV], float (&e)[kScanV],
-                                          float (&u)[kScanV]) {
+__device__ __forceinline__ float input(const FwdTile<TS>& t, int j) {
+  return get(t.x1, j) * get(t.v, j);
+}
+
+// The span of a lane's eight positions, and their decays.
+template <typename TS>
+__device__ __forceinline__ Span lane_span(const FwdTile<TS>& t, float (&e)[kScanV]) {
   Span sp = {0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < kScanV; ++j) {
-    decay(get(t.la, j), j < n, &s[j], &e[j]);
-    u[j] = j < n ? get(t.x1, j) * get(t.v, j) : 0.f;
-    sp.u = advance(s[j], e[j], sp.u, u[j]);
-    sp.s += s[j];
+    const float s = decay(get(t.la, j));
+    e[j] = pow2f(s);
+    sp.u = advance(e[j], sp.u, input(t, j));
+    sp.s += s;
   }
   return sp;
 }
 
-// G lanes a row (G < 64: a row is one tile), W wavefronts a row.
-template <typename TS, int G, int W>
-__global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_forward(ScanArgs a) {
+// G lanes a row (G < 64: a row is one tile), W wavefronts a row, or (LINKED) a
+// segment of one.
+template <typename TS, int G, int W, bool LINKED>
+__global__ void __launch_bounds__(W > 4 ? 64 * W : 256) scan_forward(ScanArgs a) {
   __shared__ Span joint[2][W > 1 ? W : 1];
-  const Place<G, W> at(a.R);
+  const uint32_t group = LINKED ? link_row(a) : blockIdx.x, seg = LINKED ? link_draw(a, group) : 0;
+  const Place<G, W> at(a.R, group);
   const int64_t len = row_length(a, at.row), base = at.row * a.L;
   const float D = ld1(reinterpret_cast<const TS*>(a.D) + (uint32_t)at.row % (uint32_t)a.C);
-  const int64_t seg = blockIdx.y, first = seg * a.seg_tiles;
-  const int64_t ntiles = G < 64 ? 1 : (a.L + kScanTile - 1) / kScanTile;
-  const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
-  float h = a.seg_in ? a.seg_in[at.row * a.nseg + seg] : (a.h0 ? a.h0[at.row] : 0.f);
+  const int64_t ntiles = G < 64 ? 1 : (a.L + kScanTile - 1) / kScanTile, first = (int64_t)seg * W;
+  const int64_t end = LINKED && first + W < ntiles ? first + W : ntiles;
+  float h = a.h0 ? a.h0[at.row] : 0.f;
   const int64_t in_tile = (int64_t)(at.lane & (G - 1)) * kScanV;
   const int64_t wave = W > 1 ? at.wave : 0;
   auto pos = [&](int64_t tile) { return (tile + wave) * kScanTile + in_tile; };
   auto count = [&](int64_t tile) { return tile + wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
   FwdTile<TS> cur, nxt;
-  load_fwd<TS, true>(cur, a, base + pos(first), count(first));
+  load_fwd(cur, a, base + pos(first), count(first));
   int buf = 0;
   for (int64_t tile = first; tile < end; tile += W) {
     const int64_t p = pos(tile);
     const int n = count(tile);
-    if (tile + W < end) load_fwd<TS, true>(nxt, a, base + pos(tile + W), count(tile + W));
-    float s[kScanV], e[kScanV], u[kScanV], y[kScanV];
-    const Span lanes = prefix<G>(lane_span(cur, n, s, e, u), at.lane);
+    if (!LINKED && tile + W < end) load_fwd(nxt, a, base + pos(tile + W), count(tile + W));
+    float e[kScanV], y[kScanV];
+    const Span lanes = prefix<G>(lane_span(cur, e), at.lane);
+    keep_packed(cur.x1);
+    keep_packed(cur.v);
     Span in = below<G>(lanes, at.lane), all;
     float h_tile = h;  // the state that enters this wavefront's tile
     if constexpr (W > 1) {
-      h_tile = through(across_waves<W>({read_lane(lanes.s, 63), read_lane(lanes.u, 63)}, joint[buf], at.wave, at.lane, &all), h);
+      const Span before = across_waves<W>({read_lane(lanes.s, 63), read_lane(lanes.u, 63)}, joint[buf], at.wave, at.lane, &all);
+      if constexpr (LINKED) {
+        __shared__ float entered;
+        if (at.wave == 0) {
+          const float x = link_enter(a.links + 2 * at.row * a.nseg, seg, all, h, at.lane);
+          if (at.lane == 0) entered = x;
+        }
+        __syncthreads();
+        h = entered;
+      }
+      h_tile = through(before, h);
       buf ^= 1;
     }
     float x = through(in, h_tile);
     if (a.states && at.live && (at.lane & (G - 1)) == 0 && tile + wave < end) a.states[at.row * a.nst + tile + wave] = h_tile;
 #pragma unroll
     for (int j = 0; j < kScanV; ++j) {
-      x = advance(s[j], e[j], x, u[j]);
-      y[j] = j < n ? get(cur.x2, j) * fmaf(D, u[j], x) : 0.f;
+      const float u = input(cur, j);
+      x = advance(e[j], x, u);
+      y[j] = get(cur.x2, j) * fmaf(D, u, x);
     }
+    only(y, n);
     if (at.live && tile + wave < end) store(reinterpret_cast<TS*>(a.y) + base + p, y, clamp_count<kScanV>(a.L - p));
     if constexpr (G < 64) {
       if (a.h_last && at.live && (at.lane & (G - 1)) == G - 1) a.h_last[at.row] = x;
@@ -95,68 +108,35 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_forward(ScanArgs a)
     } else {
       h = through(all, h);
     }
-    cur = nxt;
+    if (!LINKED) cur = nxt;
   }
   if constexpr (G == 64) {
     if (a.h_last && at.live && end == ntiles && wave == 0 && at.lane == 0) a.h_last[at.row] = h;
   }
 }
 
-// What each segment of a row does to a state that passes through it.
-template <typename TS, int W>
-__global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_segment(ScanArgs a) {
-  __shared__ Span joint[2][W];
-  const Place<64, W> at(a.R);
-  const int64_t len = row_length(a, at.row), base = at.row * a.L;
-  const int64_t seg = blockIdx.y, first = seg * a.seg_tiles;
-  const int64_t ntiles = (a.L + kScanTile - 1) / kScanTile;
-  const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
-  const int64_t in_tile = (int64_t)at.lane * kScanV;
-  auto pos = [&](int64_t tile) { return (tile + at.wave) * kScanTile + in_tile; };
-  auto count = [&](int64_t tile) { return tile + at.wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
-  Span sum = {0.f, 0.f};
-  FwdTile<TS> cur, nxt;
-  load_fwd<TS, false>(cur, a, base + pos(first), count(first));
-  int buf = 0;
-  for (int64_t tile = first; tile < end; tile += W) {
-    const int n = count(tile);
-    if (tile + W < end) load_fwd<TS, false>(nxt, a, base + pos(tile + W), count(tile + W));
-    float s[kScanV], e[kScanV], u[kScanV];
-    const Span lanes = prefix<64>(lane_span(cur, n, s, e, u), at.lane);
-    Span all;
-    across_waves<W>({read_lane(lanes.s, 63), read_lane(lanes.u, 63)}, joint[buf], at.wave, at.lane, &all);
-    buf ^= 1;
-    sum = then(sum, all);
-    cur = nxt;
-  }
-  if (threadIdx.x == 0) a.seg[at.row * a.nseg + seg] = make_float2(sum.s, sum.u);
-}
-
-// The state that enters each segment, a wavefront a row.
-__global__ void __launch_bounds__(256) scan_join(ScanArgs a) {
-  const Place<64, 1> at(a.R);
-  const float2 m = at.lane < a.nseg ? a.seg[at.row * a.nseg + at.lane] : make_float2(0.f, 0.f);
-  const Span in = below<64>(prefix<64>({m.x, m.y}, at.lane), at.lane);
-  if (at.live && at.lane < a.nseg) a.seg_in[at.row * a.nseg + at.lane] = through(in, a.h0 ? a.h0[at.row] : 0.f);
+__global__ void __launch_bounds__(256) scan_clear_links(uint64_t* links, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) links[i] = 0;
 }
 
 template <typename TS, int W>
 hipError_t forward_rows(const ScanArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(W > 1 ? a.R : (a.R + 3) / 4), (unsigned)a.nseg), block(W > 4 ? 64 * W : 256);
-  if constexpr (W == 16) {
-    if (a.nseg > 1) {
-      hipLaunchKernelGGL((scan_segment<TS, W>), grid, block, 0, s, a);
-      hipLaunchKernelGGL(scan_join, dim3((unsigned)((a.R + 3) / 4)), dim3(256), 0, s, a);
-    }
+  const dim3 block(W > 4 ? 64 * W : 256);
+  if (W == kLinkedWaves && a.nseg > 1) {
+    const hipError_t e = launch_scan_links(a, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((scan_forward<TS, 64, kLinkedWaves, true>), dim3((unsigned)(a.R * a.nseg)), block, 0, s, a);
+  } else {
+    hipLaunchKernelGGL((scan_forward<TS, 64, W, false>), dim3((unsigned)(W > 1 ? a.R : (a.R + 3) / 4)), block, 0, s, a);
   }
-  hipLaunchKernelGGL((scan_forward<TS, 64, W>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
 template <typename TS, int G>
 hipError_t forward_short(const ScanArgs& a, hipStream_t s) {
   const int64_t rows = 4 * (64 / G);
-  hipLaunchKernelGGL((scan_forward<TS, G, 1>), dim3((unsigned)((a.R + rows - 1) / rows)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((scan_forward<TS, G, 1, false>), dim3((unsigned)((a.R + rows - 1) / rows)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -172,7 +152,7 @@ hipError_t forward(const ScanArgs& a, const ScanShape& p, hipStream_t s) {
     default: break;
   }
   if (p.waves == 1) return forward_rows<TS, 1>(a, s);
-  return p.waves == 4 ? forward_rows<TS, 4>(a, s) : forward_rows<TS, 16>(a, s);
+  return p.waves == 4 ? forward_rows<TS, 4>(a, s) : forward_rows<TS, 8>(a, s);
 }
 
 constexpr int kStepNT = 256;
@@ -210,10 +190,9 @@ __global__ void __launch_bounds__(kStepNT) scan_step(ScanStepArgs a) {
       const int64_t i = b * a.C + c;
       float y = 0.f;
       if (in_pool) {
-        float s, e;
-        decay(ld1(reinterpret_cast<const TS*>(a.la) + i), true, &s, &e);
+        const float e = pow2f(decay(ld1(reinterpret_cast<const TS*>(a.la) + i)));
         const float u = ld1(reinterpret_cast<const TS*>(a.x1) + i) * ld1(reinterpret_cast<const TS*>(a.v) + i);
-        h = advance(s, e, h, u);
+        h = advance(e, h, u);
         y = ld1(reinterpret_cast<const TS*>(a.x2) + i) * fmaf(ld1(reinterpret_cast<const TS*>(a.D) + c), u, h);
       }
       st1(reinterpret_cast<TS*>(a.y) + i, y);
@@ -234,49 +213,47 @@ __global__ void __launch_bounds__(kStepNT) scan_step(ScanStepArgs a) {
 
 }  // namespace
 
-ScanShape scan_shape(int64_t R, int64_t L, bool backward) {
-  ScanShape p = {64, 1, 1, 0};
+// Eight wavefronts a row as long as the rows alone do not fill the chip (256 rows of
+// 65536 backward, bf16: 56 us against 71 with four and 222 with one), four from 1024 rows
+// on (1024 of 16384 backward, bf16: 57 against 58 and 70 us), one from 4096 (4096 of 4096:
+// 58 against 61 us with four).  Rows so few that most CUs would have none are split into
+// linked segments, from the length on where these pay for their two more steps (128
+// rows backward, fp32: 130 against 163 us for 2^17 positions, 39 against 45 us for 2^15, 32
+// against 28 us for 2^14; 200 rows: equal).
+ScanShape scan_shape(int64_t R, int64_t L) {
+  ScanShape p = {64, 1, 1};
   const int64_t tiles = (L + kScanTile - 1) / kScanTile;
-  p.seg_tiles = tiles;
   if (L <= 32 * kScanV) {
     p.lanes = 1;
     while (p.lanes * kScanV < L) p.lanes *= 2;
     return p;
   }
-  if (R < 2048 && tiles > 1) p.waves = R < 512 && tiles > 4 ? 16 : 4;
-  if (p.waves == 16 && R < 128) {
-    int64_t n = (256 + R - 1) / R;  // a workgroup a CU at least
-    if (n > kScanMaxSeg) n = kScanMaxSeg;
-    if (n > tiles / 16) n = tiles / 16;
-    if (n > 1) {
-      p.seg_tiles = ((tiles + n - 1) / n + 15) / 16 * 16;
-      p.nseg = (int)((tiles + p.seg_tiles - 1) / p.seg_tiles);
-    }
+  if (tiles > 1 && R < 4096) p.waves = R < 1024 && tiles > 4 ? 8 : 4;
+  if (R < 192 && tiles > 32 && R * tiles < (int64_t(1) << 24)) {  // (fewer than 2^32 work-items)
+    p.waves = kLinkedWaves;
+    p.nseg = (int)((tiles + kLinkedWaves - 1) / kLinkedWaves);
   }
-  (void)backward;
   return p;
 }
 
-size_t scan_segment_bytes(const ScanShape& p, int64_t R) {
-  return p.nseg > 1 ? (size_t)R * p.nseg * (sizeof(float2) + sizeof(float)) : 0;
-}
+size_t scan_link_bytes(const ScanShape& p, int64_t R) { return p.nseg > 1 ? ((size_t)R * (p.nseg * 2 + kLinkStride)) * sizeof(uint64_t) : 0; }
 
 size_t scan_workspace_bytes(int64_t R, int64_t L, bool backward) {
-  const ScanShape p = scan_shape(R, L, backward);
-  return scan_segment_bytes(p, R) + (backward ? (size_t)R * p.nseg * sizeof(double) : 0);
+  const ScanShape p = scan_shape(R, L);
+  return scan_link_bytes(p, R) + (backward ? (size_t)R * p.nseg * sizeof(double) : 0);
+}
+
+hipError_t launch_scan_links(const ScanArgs& a, hipStream_t s) {
+  const int64_t n = a.R * (2 * a.nseg + kLinkStride);
+  hipLaunchKernelGGL(scan_clear_links, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a.links, n);
+  return hipGetLastError();
 }
 
 hipError_t launch_scan(const ScanArgs& args, void* ws, hipStream_t s) {
   ScanArgs a = args;
-  const ScanShape p = scan_shape(a.R, a.L, false);
+  const ScanShape p = scan_shape(a.R, a.L);
   a.nseg = p.nseg;
-  a.seg_tiles = p.seg_tiles;
-  a.seg = nullptr;
-  a.seg_in = nullptr;
-  if (p.nseg > 1) {
-    a.seg = reinterpret_cast<float2*>(ws);
-    a.seg_in = reinterpret_cast<float*>(a.seg + a.R * p.nseg);
-  }
+  a.links = reinterpret_cast<uint64_t*>(ws);
   return a.bf16 ? forward<uint16_t>(a, p, s) : forward<float>(a, p, s);
 }
 

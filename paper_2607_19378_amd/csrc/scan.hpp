@@ -7,7 +7,6 @@ namespace hyenand {
 
 constexpr int kScanV = 8;                // consecutive positions of a lane
 constexpr int kScanTile = 64 * kScanV;   // positions of a wavefront's tile, and between two kept states
-constexpr int64_t kScanMaxSeg = 64;      // segments of a split row: one lane each when they are joined
 
 // One validated call.  R = B * C rows of L positions; row r belongs to sample r / C and channel r % C.
 struct ScanArgs {
@@ -26,21 +25,22 @@ struct ScanArgs {
   void *gx1, *gx2, *gv, *gla, *gD;
   float* gh0;            // [R] or null
   double* partial;       // [R * nseg] sums of gz u, then added over b and segments into gD
-  // set by the launchers: a row's tiles are split into nseg segments of seg_tiles
+  // set by the launchers: where rows are split, into nseg segments of one tile a wavefront
   int nseg;
-  int64_t seg_tiles;
-  float2* seg;           // [R * nseg] what a segment does to a state passing through: (log2 decay, sum)
-  float* seg_in;         // [R * nseg] the state that enters it
+  uint64_t* links;       // 2 words a segment (see scan_device.hpp), then each row's next segment to take
 };
 
+constexpr int64_t kLinkStride = 16;  // words between the rows' counters: a cache line each
+constexpr int kLinkedWaves = 8;  // wavefronts, and tiles, of a segment
+
 // How a call's rows are spread: lanes of a row (under 64: the row is one tile of lanes * kScanV positions), wavefronts
-// of a row, segments of a row and their tiles.
+// of a row, segments of a row (1: the wavefronts go through the whole row).
 struct ScanShape {
   int lanes, waves, nseg;
-  int64_t seg_tiles;
 };
-ScanShape scan_shape(int64_t R, int64_t L, bool backward);
-size_t scan_segment_bytes(const ScanShape& p, int64_t R);  // workspace of a split call's segments
+ScanShape scan_shape(int64_t R, int64_t L);
+size_t scan_link_bytes(const ScanShape& p, int64_t R);  // workspace of a split call's segments
+hipError_t launch_scan_links(const ScanArgs& a, hipStream_t s);  // clears them
 size_t scan_workspace_bytes(int64_t R, int64_t L, bool backward);
 hipError_t launch_scan(const ScanArgs& a, void* ws, hipStream_t s);
 hipError_t launch_scan_backward(const ScanArgs& a, void* ws, hipStream_t s);

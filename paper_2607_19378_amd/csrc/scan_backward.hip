@@ -31,24 +31,19 @@ __device__ __forceinline__ void load_bwd(BwdTile<TS>& t, const ScanArgs& a, int6
   t.gy = load(reinterpret_cast<const TS*>(a.gy) + off, n);
 }
 
-__device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
-  if (!a.len) return a.L;
-  const int64_t n = a.len[(uint32_t)row / (uint32_t)a.C];
-  return n < 0 ? 0 : (n > a.L ? a.L : n);
-}
-
 template <int G>
 __device__ __forceinline__ Span mirror(Span x) {
   if constexpr (G == 1) return x;
   return {__shfl_xor(x.s, G - 1), __shfl_xor(x.u, G - 1)};
 }
 
-// c of a lane's eight positions when nothing comes from behind
-__device__ __forceinline__ float lane_back(const float (&s)[kScanV], const float (&e)[kScanV], const float (&gz)[kScanV]) {
-  float c = 0.f;
-#pragma unroll
-  for (int j = kScanV - 1; j >= 0; --j) c = s[j] == neg_inf() ? 0.f : e[j] * (gz[j] + c);
-  return c;
+template <typename TS>
+__device__ __forceinline__ float input(const BwdTile<TS>& t, int j) {
+  return get(t.x1, j) * get(t.v, j);
+}
+template <typename TS>
+__device__ __forceinline__ float grad_z(const BwdTile<TS>& t, int j) {
+  return get(t.gy, j) * get(t.x2, j);
 }
 
 __device__ __forceinline__ double sum_lanes(double x, int lanes) {
@@ -56,18 +51,20 @@ __device__ __forceinline__ double sum_lanes(double x, int lanes) {
   return x;
 }
 
-// G lanes a row (G < 64: a row is one tile), W wavefronts a row.
-template <typename TS, int G, int W>
-__global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs a) {
+// G lanes a row (G < 64: a row is one tile), W wavefronts a row, or (LINKED) a
+// segment of one.
+template <typename TS, int G, int W, bool LINKED>
+__global__ void __launch_bounds__(W > 4 ? 64 * W : 256, LINKED ? 4 : 1) scan_gradients(ScanArgs a) {
   __shared__ Span joint[2][W > 1 ? W : 1];
   __shared__ double sums[W];
-  const Place<G, W> at(a.R);
+  const uint32_t group = LINKED ? link_row(a) : blockIdx.x, turn = LINKED ? link_draw(a, group) : 0;
+  const uint32_t seg = LINKED ? a.nseg - 1 - turn : 0;
+  const Place<G, W> at(a.R, group);
   const int64_t len = row_length(a, at.row), base = at.row * a.L;
   const float D = ld1(reinterpret_cast<const TS*>(a.D) + (uint32_t)at.row % (uint32_t)a.C);
-  const int64_t seg = blockIdx.y, first = seg * a.seg_tiles;
-  const int64_t ntiles = G < 64 ? 1 : (a.L + kScanTile - 1) / kScanTile;
-  const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
-  float c = a.seg_in ? a.seg_in[at.row * a.nseg + seg] : (a.gh_last ? a.gh_last[at.row] : 0.f);
+  const int64_t ntiles = G < 64 ? 1 : (a.L + kScanTile - 1) / kScanTile, first = (int64_t)seg * W;
+  const int64_t end = LINKED && first + W < ntiles ? first + W : ntiles;
+  float c = a.gh_last ? a.gh_last[at.row] : 0.f;
   const int64_t in_tile = (int64_t)(at.lane & (G - 1)) * kScanV;
   const int64_t wave = W > 1 ? at.wave : 0;
   auto pos = [&](int64_t tile) { return (tile + wave) * kScanTile + in_tile; };
@@ -83,52 +80,77 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
     const int64_t p = pos(tile), off = base + p;
     const int n = count(tile);
     const int w = at.live && tile + wave < end ? clamp_count<kScanV>(a.L - p) : 0;
-    if (tile > first) {
+    if (!LINKED && tile > first) {
       load_bwd(nxt, a, base + pos(tile - W), count(tile - W));
       h_nxt = state(tile - W);
     }
-    float s[kScanV], e[kScanV], u[kScanV], gz[kScanV], before[kScanV], out[kScanV];
+    float e[kScanV], before[kScanV], out[kScanV];
     Span sp = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < kScanV; ++j) {
-      decay(get(cur.la, j), j < n, &s[j], &e[j]);
-      u[j] = j < n ? get(cur.x1, j) * get(cur.v, j) : 0.f;
-      gz[j] = j < n ? get(cur.gy, j) * get(cur.x2, j) : 0.f;
-      sp.u = advance(s[j], e[j], sp.u, u[j]);
-      sp.s += s[j];
+      const float s = decay(get(cur.la, j));
+      e[j] = pow2f(s);
+      sp.u = advance(e[j], sp.u, input(cur, j));
+      sp.s += s;
     }
+    keep_packed(cur.x1);
+    keep_packed(cur.v);
     // the states, from the one before the tile on
     float x = through(below<G>(prefix<G>(sp, at.lane), at.lane), h_cur);
     float dsum = 0.f;
 #pragma unroll
     for (int j = 0; j < kScanV; ++j) {
+      const float u = input(cur, j);
       before[j] = x;
-      x = advance(s[j], e[j], x, u[j]);
-      out[j] = j < n ? get(cur.gy, j) * fmaf(D, u[j], x) : 0.f;
-      dsum = fmaf(gz[j], u[j], dsum);
+      x = advance(e[j], x, u);
+      out[j] = get(cur.gy, j) * fmaf(D, u, x);
+      dsum = fmaf(grad_z(cur, j), u, dsum);
     }
     gD += dsum;
+    only(out, n);
     store(reinterpret_cast<TS*>(a.gx2) + off, out, w);
+    keep_packed(cur.x1);
+    keep_packed(cur.v);
+    keep_packed(cur.gy);
+    keep_packed(cur.x2);
     // c, from behind: the lanes in reverse order
-    const Span back = prefix<G>(mirror<G>({sp.s, lane_back(s, e, gz)}), at.lane);
+    float back_u = 0.f;
+#pragma unroll
+    for (int j = kScanV - 1; j >= 0; --j) back_u = advance(e[j], grad_z(cur, j) + back_u, 0.f);
+    keep_packed(cur.gy);
+    keep_packed(cur.x2);
+    const Span back = prefix<G>(mirror<G>({sp.s, back_u}), at.lane);
     Span all = {0.f, 0.f};
     float c_tile = c;
     if constexpr (W > 1) {
-      c_tile = through(across_waves<W>({read_lane(back.s, 63), read_lane(back.u, 63)}, joint[buf], W - 1 - at.wave, at.lane, &all), c);
+      const Span behind = across_waves<W>({read_lane(back.s, 63), read_lane(back.u, 63)}, joint[buf], W - 1 - at.wave, at.lane, &all);
+      if constexpr (LINKED) {
+        __shared__ float entered;
+        if (at.wave == 0) {
+          const float from = link_enter(a.links + 2 * at.row * a.nseg, turn, all, c, at.lane);
+          if (at.lane == 0) entered = from;
+        }
+        __syncthreads();
+        c = entered;
+      }
+      c_tile = through(behind, c);
       buf ^= 1;
     }
     float g = through(mirror<G>(below<G>(back, at.lane)), c_tile);
     float gx1[kScanV], gv[kScanV];
 #pragma unroll
     for (int j = kScanV - 1; j >= 0; --j) {
-      const bool start = s[j] == neg_inf();
-      g += gz[j];
-      const float gu = fmaf(D, gz[j], g);
-      gx1[j] = j < n ? gu * get(cur.v, j) : 0.f;
-      gv[j] = j < n ? gu * get(cur.x1, j) : 0.f;
-      g = start ? 0.f : e[j] * g;
-      out[j] = j < n && !start ? g * before[j] : 0.f;
+      const float gz = grad_z(cur, j);
+      g += gz;
+      const float gu = fmaf(D, gz, g);
+      gx1[j] = gu * get(cur.v, j);
+      gv[j] = gu * get(cur.x1, j);
+      g = advance(e[j], g, 0.f);
+      out[j] = e[j] == 0.f ? 0.f : g * before[j];
     }
+    only(gx1, n);
+    only(gv, n);
+    only(out, n);
     store(reinterpret_cast<TS*>(a.gx1) + off, gx1, w);
     store(reinterpret_cast<TS*>(a.gv) + off, gv, w);
     store(reinterpret_cast<TS*>(a.gla) + off, out, w);
@@ -139,8 +161,10 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
     } else {
       c = through(all, c);
     }
-    cur = nxt;
-    h_cur = h_nxt;
+    if (!LINKED) {
+      cur = nxt;
+      h_cur = h_nxt;
+    }
   }
   if constexpr (G == 64) {
     if (a.gh0 && at.live && first == 0 && wave == 0 && at.lane == 0) a.gh0[at.row] = c;
@@ -152,72 +176,24 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_gradients(ScanArgs 
     gD = 0.0;
 #pragma unroll
     for (int i = 0; i < W; ++i) gD += sums[i];
-    if (threadIdx.x == 0) a.partial[at.row * a.nseg + seg] = gD;
+    if (threadIdx.x != 0) return;
   } else {
-    if (at.live && (at.lane & (G - 1)) == 0) a.partial[at.row * a.nseg + seg] = gD;
+    if (!at.live || (at.lane & (G - 1)) != 0) return;
   }
-}
-
-// What each segment of a row does to a c that passes through it, from its end.
-template <typename TS, int W>
-__global__ void __launch_bounds__(W == 16 ? 1024 : 256) scan_segment_back(ScanArgs a) {
-  __shared__ Span joint[2][W];
-  const Place<64, W> at(a.R);
-  const int64_t len = row_length(a, at.row), base = at.row * a.L;
-  const int64_t seg = blockIdx.y, first = seg * a.seg_tiles;
-  const int64_t ntiles = (a.L + kScanTile - 1) / kScanTile;
-  const int64_t end = first + a.seg_tiles < ntiles ? first + a.seg_tiles : ntiles;
-  const int64_t in_tile = (int64_t)at.lane * kScanV;
-  auto pos = [&](int64_t tile) { return (tile + at.wave) * kScanTile + in_tile; };
-  auto count = [&](int64_t tile) { return tile + at.wave < end ? clamp_count<kScanV>(len - pos(tile)) : 0; };
-  auto fetch = [&](BwdTile<TS>& t, int64_t tile) {
-    const int64_t off = base + pos(tile);
-    const int n = count(tile);
-    t.la = load(reinterpret_cast<const TS*>(a.la) + off, n);
-    t.x2 = load(reinterpret_cast<const TS*>(a.x2) + off, n);
-    t.gy = load(reinterpret_cast<const TS*>(a.gy) + off, n);
-  };
-  Span sum = {0.f, 0.f};
-  int64_t tile = first + (end - first - 1) / W * W;
-  BwdTile<TS> cur, nxt;
-  fetch(cur, tile);
-  int buf = 0;
-  for (; tile >= first; tile -= W) {
-    const int n = count(tile);
-    if (tile > first) fetch(nxt, tile - W);
-    float s[kScanV], e[kScanV], gz[kScanV], total = 0.f;
-#pragma unroll
-    for (int j = 0; j < kScanV; ++j) {
-      decay(get(cur.la, j), j < n, &s[j], &e[j]);
-      gz[j] = j < n ? get(cur.gy, j) * get(cur.x2, j) : 0.f;
-      total += s[j];
-    }
-    const Span back = prefix<64>(mirror<64>({total, lane_back(s, e, gz)}), at.lane);
-    Span all;
-    across_waves<W>({read_lane(back.s, 63), read_lane(back.u, 63)}, joint[buf], W - 1 - at.wave, at.lane, &all);
-    buf ^= 1;
-    sum = then(sum, all);
-    cur = nxt;
-  }
-  if (threadIdx.x == 0) a.seg[at.row * a.nseg + seg] = make_float2(sum.s, sum.u);
-}
-
-// The c that enters each segment from behind, a wavefront a row.
-__global__ void __launch_bounds__(256) scan_join_back(ScanArgs a) {
-  const Place<64, 1> at(a.R);
-  const int64_t i = a.nseg - 1 - at.lane;
-  const float2 m = i >= 0 ? a.seg[at.row * a.nseg + i] : make_float2(0.f, 0.f);
-  const Span in = below<64>(prefix<64>({m.x, m.y}, at.lane), at.lane);
-  if (at.live && i >= 0) a.seg_in[at.row * a.nseg + i] = through(in, a.gh_last ? a.gh_last[at.row] : 0.f);
+  if (!LINKED && a.R == a.C)
+    st1(reinterpret_cast<TS*>(a.gD) + at.row, (float)gD);  // one sample: the whole sum
+  else
+    a.partial[at.row * a.nseg + seg] = gD;
 }
 
 // gD[c]: the rows' sums in a fixed order, a workgroup a channel.
 template <typename TS>
 __global__ void __launch_bounds__(256) scan_sum_D(ScanArgs a) {
   __shared__ double part[4];
-  const int64_t c = blockIdx.x, per = a.R / a.C * a.nseg;
+  const uint32_t c = blockIdx.x, nseg = a.nseg, per = (uint32_t)a.R / a.C * nseg;
   double x = 0.0;
-  for (int64_t i = threadIdx.x; i < per; i += 256) x += a.partial[(i / a.nseg * a.C + c) * a.nseg + i % a.nseg];
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < per; i += 256) x += a.partial[((int64_t)(i / nseg) * a.C + c) * nseg + i % nseg];
   x = sum_lanes(x, 64);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -226,21 +202,21 @@ __global__ void __launch_bounds__(256) scan_sum_D(ScanArgs a) {
 
 template <typename TS, int W>
 hipError_t gradient_rows(const ScanArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(W > 1 ? a.R : (a.R + 3) / 4), (unsigned)a.nseg), block(W > 4 ? 64 * W : 256);
-  if constexpr (W == 16) {
-    if (a.nseg > 1) {
-      hipLaunchKernelGGL((scan_segment_back<TS, W>), grid, block, 0, s, a);
-      hipLaunchKernelGGL(scan_join_back, dim3((unsigned)((a.R + 3) / 4)), dim3(256), 0, s, a);
-    }
+  const dim3 block(W > 4 ? 64 * W : 256);
+  if (W == kLinkedWaves && a.nseg > 1) {
+    const hipError_t e = launch_scan_links(a, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((scan_gradients<TS, 64, kLinkedWaves, true>), dim3((unsigned)(a.R * a.nseg)), block, 0, s, a);
+  } else {
+    hipLaunchKernelGGL((scan_gradients<TS, 64, W, false>), dim3((unsigned)(W > 1 ? a.R : (a.R + 3) / 4)), block, 0, s, a);
   }
-  hipLaunchKernelGGL((scan_gradients<TS, 64, W>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
 template <typename TS, int G>
 hipError_t gradient_short(const ScanArgs& a, hipStream_t s) {
   const int64_t rows = 4 * (64 / G);
-  hipLaunchKernelGGL((scan_gradients<TS, G, 1>), dim3((unsigned)((a.R + rows - 1) / rows)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((scan_gradients<TS, G, 1, false>), dim3((unsigned)((a.R + rows - 1) / rows)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -254,9 +230,9 @@ hipError_t gradients(const ScanArgs& a, const ScanShape& p, hipStream_t s) {
     case 8: err = gradient_short<TS, 8>(a, s); break;
     case 16: err = gradient_short<TS, 16>(a, s); break;
     case 32: err = gradient_short<TS, 32>(a, s); break;
-    default: err = p.waves == 1 ? gradient_rows<TS, 1>(a, s) : (p.waves == 4 ? gradient_rows<TS, 4>(a, s) : gradient_rows<TS, 16>(a, s));
+    default: err = p.waves == 1 ? gradient_rows<TS, 1>(a, s) : (p.waves == 4 ? gradient_rows<TS, 4>(a, s) : gradient_rows<TS, 8>(a, s));
   }
-  if (err != hipSuccess) return err;
+  if (err != hipSuccess || (a.R == a.C && a.nseg == 1)) return err;
   hipLaunchKernelGGL((scan_sum_D<TS>), dim3((unsigned)a.C), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -265,16 +241,10 @@ hipError_t gradients(const ScanArgs& a, const ScanShape& p, hipStream_t s) {
 
 hipError_t launch_scan_backward(const ScanArgs& args, void* ws, hipStream_t s) {
   ScanArgs a = args;
-  const ScanShape p = scan_shape(a.R, a.L, true);
+  const ScanShape p = scan_shape(a.R, a.L);
   a.nseg = p.nseg;
-  a.seg_tiles = p.seg_tiles;
-  a.seg = nullptr;
-  a.seg_in = nullptr;
-  a.partial = reinterpret_cast<double*>(ws);
-  if (p.nseg > 1) {
-    a.seg = reinterpret_cast<float2*>(a.partial + a.R * p.nseg);
-    a.seg_in = reinterpret_cast<float*>(a.seg + a.R * p.nseg);
-  }
+  a.links = reinterpret_cast<uint64_t*>(ws);
+  a.partial = reinterpret_cast<double*>(reinterpret_cast<char*>(ws) + scan_link_bytes(p, a.R));
   return a.bf16 ? gradients<uint16_t>(a, p, s) : gradients<float>(a, p, s);
 }
 

@@ -23,10 +23,11 @@ constexpr float kStart = -87.f;  // log_a below this (a < 2^-125) starts a seque
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float pow2f(float s) { return __builtin_amdgcn_exp2f(s); }
 
-// a x + u, and u alone where s = log2 a marks a start
-__device__ __forceinline__ float advance(float s, float a, float x, float u) {
+// a x + u, and u alone where a = 0, which only a start has: a decay that is none
+// is 2^-126 at least
+__device__ __forceinline__ float advance(float a, float x, float u) {
   const float r = fmaf(a, x, u);
-  return s == neg_inf() ? u : r;
+  return a == 0.f ? u : r;
 }
 
 struct Span {
@@ -35,10 +36,14 @@ struct Span {
 
 // first, then second
 __device__ __forceinline__ Span then(Span first, Span second) {
-  return {first.s + second.s, advance(second.s, pow2f(second.s), first.u, second.u)};
+  const float r = fmaf(pow2f(second.s), first.u, second.u);
+  return {first.s + second.s, second.s == neg_inf() ? second.u : r};
 }
 
-__device__ __forceinline__ float through(Span sp, float x) { return advance(sp.s, pow2f(sp.s), x, sp.u); }
+__device__ __forceinline__ float through(Span sp, float x) {
+  const float r = fmaf(pow2f(sp.s), x, sp.u);
+  return sp.s == neg_inf() ? sp.u : r;
+}
 
 // DPP move; lanes without a source (or in a row that row_mask leaves out) get 0
 template <int CTRL, int ROWS = 0xf>
@@ -101,12 +106,102 @@ __device__ __forceinline__ Span across_waves(Span mine, Span* at, int wave, int 
   return {read_lane(x.s, wave - 1), read_lane(x.u, wave - 1)};
 }
 
-// log2 a and a of element j; behind the sample's end (j >= n) the state stays as it is
-__device__ __forceinline__ void decay(float la, bool live, float* s, float* e) {
-  float t = la < kStart ? neg_inf() : la * kLog2e;
-  t = live ? t : 0.f;
-  *s = t;
-  *e = pow2f(t);
+// log2 a; behind a sample's end, where log_a is loaded as 0, the state stays as it is
+__device__ __forceinline__ float decay(float la) { return la < kStart ? neg_inf() : la * kLog2e; }
+
+// zeros behind a sample's end, where the state goes on
+__device__ __forceinline__ void only(float (&x)[kScanV], int n) {
+  if (n < kScanV)
+#pragma unroll
+    for (int j = 0; j < kScanV; ++j) x[j] = j < n ? x[j] : 0.f;
+}
+
+__device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
+  if (!a.len) return a.L;
+  const int64_t n = a.len[(uint32_t)row / (uint32_t)a.C];
+  return n < 0 ? 0 : (n > a.L ? a.L : n);
+}
+
+// Segments of a split row are taken by workgroups of one launch, each of which
+// reads its inputs once and holds them while it learns the state that enters it.
+// A workgroup draws its segment from its row's counter, so that every segment before
+// its own in the row is finished or being worked on.  It publishes what its segment does to a state (its span) before it waits for
+// anything, then looks for the nearest segment before it that has published the
+// state behind it, and takes the spans between from there on in their order, so
+// that the roundings do not depend on the timing.  Each wait ends: a row's first
+// segment waits for nothing, and each other one for segments that are being worked on.
+//
+// Two words a segment, each written at once with its flag in the upper half:
+// word 0 (kSpan, s); word 1 (kSpan, u), later (kState, the state behind it).
+constexpr uint64_t kSpan = 1, kState = 2;
+
+__device__ __forceinline__ uint64_t link_word(uint64_t flag, float x) { return flag << 32 | __float_as_uint(x); }
+__device__ __forceinline__ float link_value(uint64_t w) { return __uint_as_float((uint32_t)w); }
+__device__ __forceinline__ uint64_t link_load(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void link_store(uint64_t* p, uint64_t w) {
+  __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The row that this workgroup works on; each row gets nseg of them.  Of few rows,
+// eight workgroups, one for each XCD, share one before the next eight go to the next
+// (16 rows of 2^20: 47 against 69 us forward, 81 against 106 us backward, bf16); of
+// more, neighbours take different ones (128 rows of 2^17 backward, fp32: 131 against 157 us).
+__device__ __forceinline__ uint32_t link_row(const ScanArgs& a) {
+  const uint32_t R = (uint32_t)a.R;
+  if (R >= 64) return blockIdx.x % R;
+  const uint32_t turn = blockIdx.x / (8 * R), in = blockIdx.x - turn * 8 * R, left = (uint32_t)a.nseg - 8 * turn;
+  return in / (left < 8 ? left : 8);
+}
+
+// The segment that this workgroup takes of row `row`, in the order of the recurrence.
+__device__ __forceinline__ uint32_t link_draw(const ScanArgs& a, uint32_t row) {
+  __shared__ uint32_t drawn;
+  if (threadIdx.x == 0)
+    drawn = (uint32_t)__hip_atomic_fetch_add(a.links + 2 * a.R * a.nseg + (int64_t)row * kLinkStride, (uint64_t)1,
+                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(drawn);
+}
+
+// By one wavefront: the state that enters segment `i` (in the order of the
+// recurrence) of a row whose words begin at `row`; the row starts from `start`.
+__device__ __forceinline__ float link_enter(uint64_t* row, uint32_t i, Span mine, float start, int lane) {
+  float x = start;
+  if (i > 0) {
+    if (lane == 0) {
+      link_store(row + 2 * i, link_word(kSpan, mine.s));
+      link_store(row + 2 * i + 1, link_word(kSpan, mine.u));
+    }
+    // lane l looks at segment i - 1 - l
+    const bool there = (uint32_t)lane < i;
+    const uint64_t* at = row + 2 * (there ? i - 1 - lane : 0);
+    uint64_t w = 0;
+    int from;
+    for (;;) {
+      if (there && w >> 32 != kState) w = link_load(at + 1);
+      const uint64_t done = __ballot(there && w >> 32 == kState), known = __ballot(there && w >> 32 != 0);
+      if (done) {
+        from = __builtin_ctzll(done);
+        const uint64_t between = (uint64_t(1) << from) - 1;
+        if ((known & between) == between) break;
+      }
+      __builtin_amdgcn_s_sleep(4);
+    }
+    uint64_t ws = link_word(kSpan, 0.f);
+    if (lane < from)
+      for (ws = link_load(at); ws >> 32 != kSpan; ws = link_load(at)) __builtin_amdgcn_s_sleep(1);
+    x = read_lane(link_value(w), from);
+    const float a = pow2f(link_value(ws));
+    const uint64_t starts = __ballot(link_value(ws) == neg_inf());
+    for (int l = from - 1; l >= 0; --l) {
+      const float u = read_lane(link_value(w), l), r = fmaf(read_lane(a, l), x, u);
+      x = (starts >> l) & 1 ? u : r;
+    }
+  }
+  if (lane == 0) link_store(row + 2 * i + 1, link_word(kState, through(mine, x)));
+  return x;
 }
 
 // Where a lane works: its row and the tile of a wavefront.
@@ -115,11 +210,11 @@ struct Place {
   int lane, wave;
   int64_t row;
   bool live;  // false: a lane beyond the last row, which computes on the last one and writes nothing
-  __device__ __forceinline__ explicit Place(int64_t R) {
+  __device__ __forceinline__ explicit Place(int64_t R, uint32_t group = blockIdx.x) {
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if constexpr (W > 1) {
-      row = blockIdx.x;
+      row = group;
     } else if constexpr (G == 64) {
       row = (int64_t)blockIdx.x * 4 + wave;
     } else {
