@@ -160,9 +160,13 @@ def kernel_shape(shape, pad_mode: str, shared_k: bool = False):
 
 def _dtype_code(dtype) -> int:
     import torch
-    if dtype in (torch.float32, "f32", "float32"):
+    if dtype is torch.float32:
         return DTYPE_F32
-    if dtype in (torch.bfloat16, "bf16", "bfloat16"):
+    if dtype is torch.bfloat16:
+        return DTYPE_BF16
+    if dtype in ("f32", "float32"):
+        return DTYPE_F32
+    if dtype in ("bf16", "bfloat16"):
         return DTYPE_BF16
     raise ValueError(f"unsupported dtype {dtype}")
 
@@ -647,11 +651,12 @@ class _Call:
     """A marshalled call: enqueues its work again each time it is called, on
     the same buffers and stream, which it keeps alive."""
 
-    def _prepare(self, fn, args, device, stream, keep) -> None:
+    def _prepare(self, fn, args, like, stream, keep) -> None:
         import torch
+        self._device = like.get_device()
         if stream is None:
-            stream = torch.cuda.current_stream(device)
-        self._fn, self._device = fn, device.index
+            stream = torch.cuda.current_stream(self._device)
+        self._fn = fn
         self._args = args + (stream.cuda_stream,)
         self._current = torch.cuda.current_device
         self._keep = (keep, stream)
@@ -703,14 +708,15 @@ def scan_states_shape(shape):
     return B, C, -(-L // SCAN_BLOCK)
 
 
-def _scan_inputs(x1, x2, v, log_a, D, lengths):
+def _scan_inputs(x1, D, lengths, gD=None, **like_x1):
     import torch
     if x1.dim() != 3:
         raise ValueError(f"x1 must be [B, C, L], got {tuple(x1.shape)}")
     code, shape = _gpu_dtype(x1), tuple(x1.shape)
-    _expect(x1, shape, x1.dtype, x1=x1, x2=x2, v=v, log_a=log_a)
-    _expect(x1, shape[1:2], x1.dtype, D=D)
-    _expect(x1, shape[:1], torch.int64, lengths=lengths)
+    _expect(x1, shape, x1.dtype, x1=x1, **like_x1)
+    _expect(x1, shape[1:2], x1.dtype, D=D, gD=gD)
+    if lengths is not None:
+        _expect(x1, shape[:1], torch.int64, lengths=lengths)
     return code, shape
 
 
@@ -722,14 +728,13 @@ class PreparedScan(_Call):
     def __init__(self, y, x1, x2, v, log_a, D, h0=None, lengths=None, h_last=None, states=None, workspace=None,
                  stream=None):
         import torch
-        code, shape = _scan_inputs(x1, x2, v, log_a, D, lengths)
-        _expect(x1, shape, x1.dtype, y=y)
+        code, shape = _scan_inputs(x1, D, lengths, x2=x2, v=v, log_a=log_a, y=y)
         _expect(x1, shape[:2], torch.float32, h0=h0, h_last=h_last)
         _expect(x1, scan_states_shape(shape), torch.float32, states=states)
         ws, ws_ptr, ws_bytes = _scratch(scan_workspace_size(shape, x1.dtype), workspace, x1.device, stream)
         self._prepare(lib().hyenand_scan,
                       _pointers(x1, x2, v, log_a, D, h0, lengths, y, h_last, states) + shape + (code, ws_ptr, ws_bytes),
-                      x1.device, stream,
+                      x1, stream,
                       (y, x1, x2, v, log_a, D, h0, lengths, h_last, states, ws))
 
 
@@ -754,15 +759,14 @@ class PreparedScanBackward(_Call):
     def __init__(self, gx1, gx2, gv, glog_a, gD, gh0, x1, x2, v, log_a, D, states, gy, lengths=None, gh_last=None,
                  workspace=None, stream=None):
         import torch
-        code, shape = _scan_inputs(x1, x2, v, log_a, D, lengths)
-        _expect(x1, shape, x1.dtype, gy=gy, gx1=gx1, gx2=gx2, gv=gv, glog_a=glog_a)
-        _expect(x1, shape[1:2], x1.dtype, gD=gD)
+        code, shape = _scan_inputs(x1, D, lengths, gD, x2=x2, v=v, log_a=log_a, gy=gy, gx1=gx1, gx2=gx2, gv=gv,
+                                   glog_a=glog_a)
         _expect(x1, shape[:2], torch.float32, gh_last=gh_last, gh0=gh0)
         _expect(x1, scan_states_shape(shape), torch.float32, states=states)
         ws, ws_ptr, ws_bytes = _scratch(scan_backward_workspace_size(shape, x1.dtype), workspace, x1.device, stream)
         self._prepare(lib().hyenand_scan_backward,
                       _pointers(x1, x2, v, log_a, D, lengths, states, gy, gh_last, gx1, gx2, gv, glog_a, gD, gh0)
-                      + shape + (code, ws_ptr, ws_bytes), x1.device, stream,
+                      + shape + (code, ws_ptr, ws_bytes), x1, stream,
                       (gx1, gx2, gv, glog_a, gD, gh0, x1, x2, v, log_a, D, states, gy, lengths, gh_last, ws))
 
 
@@ -794,7 +798,7 @@ class PreparedScanStep(_Call):
         _expect(x1, (state.shape[0], shape[1]), torch.float32, state=state)
         _expect(x1, shape[:1], torch.int64, slots=slots)
         self._prepare(lib().hyenand_scan_step,
-                      _pointers(x1, x2, v, log_a, D, slots, state, y) + shape + (int(state.shape[0]), code), x1.device, stream, (y, x1, x2, v, log_a, D, state, slots))
+                      _pointers(x1, x2, v, log_a, D, slots, state, y) + shape + (int(state.shape[0]), code), x1, stream, (y, x1, x2, v, log_a, D, state, slots))
 
 
 def scan_step(x1, x2, v, log_a, D, state, slots=None, stream=None):
@@ -819,14 +823,15 @@ def block_norm_backward_workspace_size(shape, dtype) -> int:
     return _query("hyenand_block_norm_backward_workspace_size", tuple(shape), _dtype_code(dtype))
 
 
-def _norm_inputs(x, z, gate, w_post, scale, w_pre, rng):
+def _norm_inputs(x, rng, like_x, like_w):
     import torch
     code, shape = _gpu_dtype(x), tuple(x.shape)
     BCP = _points(shape)
-    _expect(x, shape, x.dtype, x=x, z=z, gate=gate)
-    _expect(x, shape[1:2], x.dtype, w_post=w_post, scale=scale, w_pre=w_pre)
-    _expect(x, (2,), torch.int64, rng=rng)
-    return code, shape, BCP
+    _expect(x, shape, x.dtype, **like_x)
+    _expect(x, shape[1:2], x.dtype, **like_w)
+    if rng is not None:
+        _expect(x, (2,), torch.int64, rng=rng)
+    return code, BCP
 
 
 class PreparedBlockNorm(_Call):
@@ -836,11 +841,11 @@ class PreparedBlockNorm(_Call):
 
     def __init__(self, x_out, n, x, z=None, gate=None, w_post=None, scale=None, w_pre=None, eps_post: float = 1e-6,
                  eps_pre: float = 1e-6, dropout_p: float = 0.0, rng=None, stream=None):
-        code, shape, BCP = _norm_inputs(x, z, gate, w_post, scale, w_pre, rng)
-        _expect(x, shape, x.dtype, x_out=x_out, n=n)
+        code, BCP = _norm_inputs(x, rng, dict(x=x, z=z, gate=gate, x_out=x_out, n=n),
+                                 dict(w_post=w_post, scale=scale, w_pre=w_pre))
         self._prepare(lib().hyenand_block_norm,
                       _pointers(x, z, gate, w_post, scale, w_pre) + (eps_post, eps_pre, dropout_p)
-                      + _pointers(rng, x_out, n) + BCP + (code,), x.device, stream, (x_out, n, x, z, gate, w_post, scale, w_pre, rng))
+                      + _pointers(rng, x_out, n) + BCP + (code,), x, stream, (x_out, n, x, z, gate, w_post, scale, w_pre, rng))
 
 
 def block_norm(x, z=None, gate=None, w_post=None, scale=None, w_pre=None, eps_post: float = 1e-6, eps_pre: float = 1e-6,
@@ -864,14 +869,13 @@ class PreparedBlockNormBackward(_Call):
     def __init__(self, gx, gz, ggate, gw_post, gscale, gw_pre, x_out, z, gate, w_post, scale, w_pre, gx_out, gn,
                  eps_post: float = 1e-6, eps_pre: float = 1e-6, dropout_p: float = 0.0, rng=None, workspace=None,
                  stream=None):
-        code, shape, BCP = _norm_inputs(x_out, z, gate, w_post, scale, w_pre, rng)
-        _expect(x_out, shape, x_out.dtype, gx_out=gx_out, gn=gn, gx=gx, gz=gz, ggate=ggate)
-        _expect(x_out, shape[1:2], x_out.dtype, gw_post=gw_post, gscale=gscale, gw_pre=gw_pre)
+        code, BCP = _norm_inputs(x_out, rng, dict(x_out=x_out, z=z, gate=gate, gx_out=gx_out, gn=gn, gx=gx, gz=gz, ggate=ggate),
+                                 dict(w_post=w_post, scale=scale, w_pre=w_pre, gw_post=gw_post, gscale=gscale, gw_pre=gw_pre))
         ws, ws_ptr, ws_bytes = _scratch(block_norm_backward_workspace_size(BCP, x_out.dtype), workspace, x_out.device,
                                         stream)
         self._prepare(lib().hyenand_block_norm_backward,
                       _pointers(x_out, z, gate, w_post, scale, w_pre) + (eps_post, eps_pre, dropout_p)
-                      + _pointers(rng, gx_out, gn, gx, gz, ggate, gw_post, gscale, gw_pre) + BCP + (code, ws_ptr, ws_bytes), x_out.device, stream,
+                      + _pointers(rng, gx_out, gn, gx, gz, ggate, gw_post, gscale, gw_pre) + BCP + (code, ws_ptr, ws_bytes), x_out, stream,
                       (gx, gz, ggate, gw_post, gscale, gw_pre, x_out, z, gate, w_post, scale, w_pre, gx_out, gn, rng, ws))
 
 
