@@ -183,16 +183,30 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
     wp[k] = Has::z(a) && c < a.C ? weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) : 0.f;
     w_pre[k] = Has::gn(a) && c < a.C ? weight<TS>(a.w_pre, c) : 0.f;
   }
-  for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
-    const uint32_t tile = tile_of(a, turn);
-    if (tile >= a.tiles) continue;
-    const Held<TS, V, Has::TAIL> at(a, tile);
-    BwdRow<TS, V> r[K];
+  // this workgroup's next tile, from turn `turn` on (a.tiles: none)
+  uint32_t turn = blockIdx.x;
+  auto next_tile = [&]() {
+    for (; turn < a.turns; turn += gridDim.x) {
+      const uint32_t tile = tile_of(a, turn);
+      if (tile < a.tiles) {
+        turn += gridDim.x;
+        return tile;
+      }
+    }
+    return a.tiles;
+  };
+  BwdRow<TS, V> r[K];
+  auto fetch = [&](const Held<TS, V, Has::TAIL>& at) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       r[k] = BwdRow<TS, V>{};
       if (first + k * CL < a.C && at.any()) load_row<Has>(r[k], a, at, k);
     }
+  };
+  uint32_t tile = next_tile();
+  if (tile < a.tiles) fetch(Held<TS, V, Has::TAIL>(a, tile));
+  while (tile < a.tiles) {
+    const Held<TS, V, Has::TAIL> at(a, tile);
     float acc[3][V], sum[1][V], gmw[K][V];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = acc[2][j] = sum[0][j] = 0.f;
@@ -206,21 +220,26 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
       keep_packed(r[k].z);
     }
     over_channels(acc, lds, a.lp, at.pg, [&](int m, float s) { return first_kind(a, m, s); });
+    Raw<TS, V> z[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float gx[V];
-      second_sums<Has>(r[k], a, draws, at.b * a.C + first + k * CL, at.p, at.shift, w_pre[k], wp[k], lds, at.pg, Gates<V>(k), gx,
-                       gmw[k], sum, &weights[k]);
+      second_sums<Has>(r[k], a, draws, at.b * a.C + first + k * CL, at.p, at.shift, w_pre[k], wp[k], lds, at.pg, Gates<V>(k),
+                       gx, gmw[k], sum, &weights[k]);
       if (first + k * CL < a.C && at.any()) at.store(a.gx, k, gx);
       keep_packed(r[k].z);
+      z[k] = r[k].z;
       next_channel();
     }
+    // the next tile's inputs come while this one's branch is finished
+    tile = next_tile();
+    if (tile < a.tiles) fetch(Held<TS, V, Has::TAIL>(a, tile));
     if (!Has::z(a)) continue;
     over_channels(sum, lds1, a.lp, at.pg, [&](int, float s) { return s / (float)a.C; });
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float gz[V], gg[V];
-      last_row<Has>(r[k].z, a, lds, lds1, at.pg, Gates<V>(k), gmw[k], gz, gg);
+      last_row<Has>(z[k], a, lds, lds1, at.pg, Gates<V>(k), gmw[k], gz, gg);
       if (first + k * CL < a.C && at.any()) {
         at.store(a.gz, k, gz);
         if (Has::g(a)) at.store(a.gg, k, gg);
@@ -327,7 +346,12 @@ __global__ void __launch_bounds__(1024) norm_weights(NormArgs a) {
   }
 }
 
-int groups_of(uint32_t turns) { return (int)(turns < 1024 ? turns : 1024); }
+// The workgroups that the chip holds at once (16 wavefronts a CU of the registers that
+// a tile takes): each goes through its share of the tiles.
+int groups_of(uint32_t turns, int NT) {
+  const uint32_t most = 256u * (NT >= 1024 ? 1 : 1024 / NT);
+  return (int)(turns < most ? turns : most);
+}
 
 template <typename TS, typename Has>
 void backward_held(const NormArgs& a, const NormShape& s, hipStream_t st) {
@@ -374,15 +398,16 @@ size_t norm_backward_workspace_bytes(int64_t B, int64_t C, int64_t P, bool bf16)
   a.B = B;
   a.C = (int)C;
   a.P = P;
-  norm_tiles(a, norm_shape(C, P, B, bf16, true));
-  return (size_t)groups_of(a.turns) * (size_t)C * sizeof(float2);
+  const NormShape s = norm_shape(C, P, B, bf16, true);
+  norm_tiles(a, s);
+  return (size_t)groups_of(a.turns, s.NT) * (size_t)C * sizeof(float2);
 }
 
 hipError_t launch_norm_backward(const NormArgs& args, hipStream_t st) {
   NormArgs a = args;
   const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, true);
   norm_tiles(a, s);
-  a.groups = groups_of(a.turns);
+  a.groups = groups_of(a.turns, s.NT);
   return a.bf16 ? backward<uint16_t>(a, s, st) : backward<float>(a, s, st);
 }
 
