@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forwar
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = first + k * CL;
-    w_post[k] = Has::z(a) && c < a.C ? weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) : 0.f;
+    w_post[k] = Has::z(a) && c < a.C ? weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) * a.kept : 0.f;
     w_pre[k] = Has::n(a) && c < a.C ? weight<TS>(a.w_pre, c) : 0.f;
   }
   for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
@@ -34,11 +34,12 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forwar
     Raw<TS, V> x[K], z[K], g[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k] = z[k] = g[k] = Raw<TS, V>{};
       if (first + k * CL < a.C && at.any()) {
         if (Has::z(a)) z[k] = at.load(a.z, k);
         if (Has::g(a)) g[k] = at.load(a.g, k);
         x[k] = at.load(a.x, k);
+      } else {
+        x[k] = z[k] = g[k] = Raw<TS, V>{};
       }
     }
     float y[K][V];  // the branch, then the sum
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forwar
           if (Has::g(a)) y[k][j] *= sigmoid_of(gate(get(g[k], j)));
           acc[0][j] = fmaf(y[k][j], y[k][j], acc[0][j]);
         }
-      over_channels(acc, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_post); });
+      over_channels(acc, lds, a.lp, at.pg, [&](int, auto sum, int) { return inverse_rms(sum(0), a.C, a.eps_post); });
       read_sums(lds, 0, at.pg, post);
     }
 #pragma unroll
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forwar
         if (Has::drop(a)) draws.words<V, Has::TAIL>(at.b * a.C + c, at.p, at.shift, drawn);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float w = Has::drop(a) ? draws.factor(drawn, j) * w_post[k] : w_post[k];
+          const float w = !Has::drop(a) || draws.keeps(drawn, j) ? w_post[k] : 0.f;
           y[k][j] = fmaf(w, y[k][j] * post[j], get(x[k], j));
         }
         if (c < a.C && at.any()) at.store(a.x_out, k, y[k]);
@@ -80,7 +81,7 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forwar
       for (int j = 0; j < V; ++j) acc[0][j] = fmaf(y[k][j], y[k][j], acc[0][j]);
     }
     if (!Has::n(a)) continue;
-    over_channels(acc, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_pre); });
+    over_channels(acc, lds, a.lp, at.pg, [&](int, auto sum, int) { return inverse_rms(sum(0), a.C, a.eps_pre); });
     read_sums(lds, 0, at.pg, post);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -121,11 +122,11 @@ __global__ void __launch_bounds__(kMaxNT) norm_forward_reread(NormArgs a) {
         return;
       }
       branch(c, y);
-      const float w = weight<TS>(a.w_post, c) * weight<TS>(a.scale, c);
+      const float w = weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) * a.kept;
       uint32_t drawn[4];
       if (a.drop) draws.words<V, false>(at.b * a.C + c, at.p, 0, drawn);
 #pragma unroll
-      for (int j = 0; j < V; ++j) y[j] = fmaf(a.drop ? draws.factor(drawn, j) * w : w, y[j] * post[0][j], get(x, j));
+      for (int j = 0; j < V; ++j) y[j] = fmaf(!a.drop || draws.keeps(drawn, j) ? w : 0.f, y[j] * post[0][j], get(x, j));
     };
 #pragma unroll
     for (int j = 0; j < V; ++j) post[0][j] = pre[0][j] = 0.f;
@@ -136,7 +137,7 @@ __global__ void __launch_bounds__(kMaxNT) norm_forward_reread(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) post[0][j] = fmaf(t[j], t[j], post[0][j]);
       }
-      over_channels(post, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_post); });
+      over_channels(post, lds, a.lp, at.pg, [&](int, auto sum, int) { return inverse_rms(sum(0), a.C, a.eps_post); });
       read_sums(lds, 0, at.pg, post[0]);
     }
     for (int c = at.cl; c < a.C; c += at.CL) {
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(kMaxNT) norm_forward_reread(NormArgs a) {
       for (int j = 0; j < V; ++j) pre[0][j] = fmaf(y[j], y[j], pre[0][j]);
     }
     if (!a.n) continue;
-    over_channels(pre, lds, a.lp, at.pg, [&](int, float s) { return inverse_rms(s, a.C, a.eps_pre); });
+    over_channels(pre, lds, a.lp, at.pg, [&](int, auto sum, int) { return inverse_rms(sum(0), a.C, a.eps_pre); });
     read_sums(lds, 0, at.pg, pre[0]);
     for (int c = at.cl; c < a.C; c += at.CL) {
       float y[V];

@@ -15,7 +15,7 @@ struct NormArgs {
   int C;
   float eps_post, eps_pre;
   uint32_t drop;                    // a point is dropped where its 16 random bits are below this
-  float kept;                       // what a kept one is multiplied by, 65536 / (65536 - drop)
+  float kept;                       // what a kept one is multiplied by, 65536 / (65536 - drop); 1 without dropout
   bool bf16;
   // backward: null where there is none
   const void *gx_out, *gn;

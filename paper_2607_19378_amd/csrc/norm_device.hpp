@@ -24,7 +24,7 @@ constexpr int kMaxLanes = 8;  // over a channel's points
 __device__ __forceinline__ float gate(float g) {
   const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(g));
   const float m = e * __builtin_amdgcn_rcpf(1.f + e);
-  return __uint_as_float(__float_as_uint(g != g ? g : m) | (g >= 0.f ? 0x80000000u : 0u));
+  return __uint_as_float(__float_as_uint(m) | (~__float_as_uint(g) & 0x80000000u));
 }
 __device__ __forceinline__ float sigmoid_of(float m) { return __float_as_int(m) < 0 ? 1.f + m : m; }
 __device__ __forceinline__ float rest_of(float m) { return __float_as_int(m) < 0 ? -m : 1.f - m; }
@@ -38,9 +38,9 @@ __device__ __forceinline__ void philox(uint64_t index, uint64_t offset, uint64_t
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+    c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);  // a ^ b ^ c
     c1 = (uint32_t)p1;
-    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+    c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c3, k1, 0x96);
     c3 = (uint32_t)p0;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -57,7 +57,6 @@ struct Draws {
   uint64_t seed, offset;
   int64_t groups;  // of a row
   uint32_t drop;
-  float kept;
   static __device__ __forceinline__ uint64_t uniform(uint64_t x) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
     return (uint64_t)hi << 32 | lo;
@@ -67,7 +66,6 @@ struct Draws {
     offset = uniform(a.drop ? a.rng[1] : 0);
     groups = (a.P + 7) / 8;
     drop = a.drop;
-    kept = a.kept;
   }
   // The draws of V points of row `row`, p the first one, a multiple of V; place j
   // has that of point j - shift.
@@ -107,10 +105,8 @@ struct Draws {
       }
     }
   }
-  // what point j is multiplied by
-  __device__ __forceinline__ float factor(const uint32_t (&w)[4], int j) const {
-    const uint32_t bits = (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xffffu;
-    return bits >= drop ? kept : 0.f;
+  __device__ __forceinline__ bool keeps(const uint32_t (&w)[4], int j) const {
+    return ((j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xffffu) >= drop;
   }
 };
 
@@ -215,7 +211,7 @@ __device__ __forceinline__ float add_halves(float a, float b) {
 }
 
 // M sums over the channels of each point of the tile.  all[m] is what finish(m,
-// sum) makes of them.
+// sum, point) makes of them; it may ask for another one of the point's sums.
 template <int M, int V>
 struct Joint {
   float part[kMaxNT / 64][M * V][kMaxLanes];
@@ -253,10 +249,14 @@ __device__ __forceinline__ void over_channels(const float (&acc)[M][V], Joint<M,
   __syncthreads();
   for (int t = threadIdx.x; t < N << lp; t += blockDim.x) {
     const int i = t >> lp, g = t & (LP - 1);
-    float sum = 0.f;
+    auto sum = [&](int m) {
+      float x = 0.f;
 #pragma unroll 4
-    for (int w = 0; w < waves; ++w) sum += lds.part[w][i][g];
-    lds.all[i / V][g * V + i % V] = finish(i / V, sum);
+      for (int w = 0; w < waves; ++w) x += lds.part[w][m * V + i % V][g];
+      return x;
+    };
+    const int m = i / V, point = g * V + i % V;
+    lds.all[m][point] = finish(m, sum, point);
   }
   __syncthreads();
 }
