@@ -248,6 +248,9 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
     for (int k = 0; k < K; ++k) {
       float gz[V], gg[V];
       last_row<Has>(a, lds, lds1, at.pg, Branch<V>(k), gmw[k], gz, gg);
+      // the next inputs are there by now, or else they would be waited for behind these
+      // stores, and with them
+      if (k == 0) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
       if (first + k * CL < a.C && at.any()) {
         at.store(a.gz, k, gz);
         if (Has::g(a)) at.store(a.gg, k, gg);
