@@ -39,7 +39,9 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_forwar
         if (Has::g(a)) g[k] = at.load(a.g, k);
         x[k] = at.load(a.x, k);
       } else {
-        x[k] = z[k] = g[k] = Raw<TS, V>{};
+        x[k] = Raw<TS, V>{};
+        z[k] = Raw<TS, V>{};
+        g[k] = Raw<TS, V>{};
       }
     }
     float y[K][V];  // the branch, then the sum
@@ -228,7 +230,7 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
   if (C * P <= (int64_t(1) << 32) / (bf16 ? 2 : 4) - 4096) {
     for (; lp >= 0; --lp) {
       if (s.V == 1) {
-        if (take(1, lp, kMaxNT) || take(4, lp, kMaxNT) || take(8, lp, kMaxNT)) return s;
+        if (take(1, lp, kMaxNT) || take(4, lp, kMaxNT) || (!backward && take(8, lp, kMaxNT))) return s;
         continue;
       }
       const bool many = (groups >> lp) * B >= 512;

@@ -27,17 +27,6 @@ struct BwdRow {
   Raw<TS, V> x, gn, gxo, z, g;
 };
 
-template <typename Has, typename TS, int V>
-__device__ __forceinline__ void load_row(BwdRow<TS, V>& r, const NormArgs& a, const Held<TS, V, Has::TAIL>& at, int k) {
-  r.x = at.load(a.x, k);
-  if (Has::gn(a)) r.gn = at.load_own(a.gn, k);
-  if (Has::z(a)) {
-    r.z = at.load(a.z, k);
-    if (Has::g(a)) r.g = at.load(a.g, k);
-  }
-  if (Has::gx_out(a)) r.gxo = at.load_own(a.gx_out, k);
-}
-
 template <typename TS, int V>
 __device__ __forceinline__ void load_row(BwdRow<TS, V>& r, const NormArgs& a, int64_t o, int n) {
   r.x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + o, n);
@@ -208,15 +197,39 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
     return a.tiles;
   };
   BwdRow<TS, V> r[K];
-  auto fetch = [&](const Held<TS, V, Has::TAIL>& at) {
+  // the inputs of a tile: of the branch, and of the stream
+  auto fetch_branch = [&](const Held<TS, V, Has::TAIL>& at) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (first + k * CL < a.C && at.any()) load_row<Has>(r[k], a, at, k);
-      else r[k] = BwdRow<TS, V>{};
+      if (first + k * CL < a.C && at.any()) {
+        if (Has::z(a)) r[k].z = at.load(a.z, k);
+        if (Has::g(a)) r[k].g = at.load(a.g, k);
+      } else {
+        if (Has::z(a)) r[k].z = Raw<TS, V>{};
+        if (Has::g(a)) r[k].g = Raw<TS, V>{};
+      }
+    }
+  };
+  auto fetch_stream = [&](const Held<TS, V, Has::TAIL>& at) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (first + k * CL < a.C && at.any()) {
+        r[k].x = at.load(a.x, k);
+        if (Has::gn(a)) r[k].gn = at.load_own(a.gn, k);
+        if (Has::gx_out(a)) r[k].gxo = at.load_own(a.gx_out, k);
+      } else {
+        r[k].x = Raw<TS, V>{};
+        if (Has::gn(a)) r[k].gn = Raw<TS, V>{};
+        if (Has::gx_out(a)) r[k].gxo = Raw<TS, V>{};
+      }
     }
   };
   uint32_t tile = next_tile();
-  if (tile < a.tiles) fetch(Held<TS, V, Has::TAIL>(a, tile));
+  if (tile < a.tiles) {
+    const Held<TS, V, Has::TAIL> at(a, tile);
+    fetch_branch(at);
+    fetch_stream(at);
+  }
   while (tile < a.tiles) {
     const Held<TS, V, Has::TAIL> at(a, tile);
     float acc[3][V], sum[1][V], gmw[K][V];
@@ -230,6 +243,9 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
       keep_packed(r[k].gn);
       keep_packed(r[k].gxo);
     }
+    // the next tile's inputs come as soon as this one's have been used
+    const uint32_t next = next_tile();
+    if (next < a.tiles) fetch_branch(Held<TS, V, Has::TAIL>(a, next));
     over_channels(acc, lds, a.lp, at.pg, [&](int m, auto sum, int) { return first_kind(a, m, sum); });
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -239,9 +255,8 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
       if (first + k * CL < a.C && at.any()) at.store(a.gx, k, gx);
       next_channel();
     }
-    // the next tile's inputs come while this one's branch is finished
-    tile = next_tile();
-    if (tile < a.tiles) fetch(Held<TS, V, Has::TAIL>(a, tile));
+    if (next < a.tiles) fetch_stream(Held<TS, V, Has::TAIL>(a, next));
+    tile = next;
     if (!Has::z(a)) continue;
     over_channels(sum, lds1, a.lp, at.pg, [&](int, auto sum, int point) { return second_kind(a, lds, point, sum(0)); });
 #pragma unroll
@@ -384,7 +399,7 @@ hipError_t backward_held(const NormArgs& a, const NormShape& s, hipStream_t st) 
 #define HY_CASE(v, k) \
   if (s.V == v && s.K == k) return launch<norm_backward<TS, v, k, Has>>(a, s.NT, lds, st);
   if constexpr (!Has::TAIL) {
-    HY_CASE(1, 1) HY_CASE(1, 4) HY_CASE(1, 8)
+    HY_CASE(1, 1) HY_CASE(1, 4)
   }
   HY_CASE(V, 1) HY_CASE(V, 2) HY_CASE(V, 4)
 #undef HY_CASE

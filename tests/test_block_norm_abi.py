@@ -64,7 +64,7 @@ def test_numbers(names):
         assert call(names, p=p) == H.ERR_INVALID_ARGUMENT and "dropout_p" in said()
     for eps in ((-1e-6, 0.0), (0.0, math.nan), (math.inf, 0.0)):
         assert call(names, eps=eps) == H.ERR_INVALID_ARGUMENT and "eps" in said()
-    for kw, st in ((dict(B=0), 1), (dict(C=-1), 1), (dict(P=0), 1), (dict(dtype=2), 1), (dict(C=1 << 22), 2), (dict(P=1 << 41), 2)):
+    for kw, st in ((dict(B=0), 1), (dict(C=-1), 1), (dict(P=0), 1), (dict(dtype=2), 1), (dict(C=1 << 26), 2), (dict(P=1 << 41), 2)):
         assert call(names, **kw) == st, kw
 
 

@@ -69,7 +69,7 @@ def test_overlapping_outputs(fn):
 @pytest.mark.parametrize("fn", list(kinds()))
 def test_shapes_and_types(fn):
     for kw, status in ((dict(B=0), H.ERR_INVALID_ARGUMENT), (dict(C=0), H.ERR_INVALID_ARGUMENT), (dict(dtype=2), H.ERR_INVALID_ARGUMENT),
-                       (dict(B=-1), H.ERR_INVALID_ARGUMENT), (dict(B=1 << 12, C=1 << 10), H.ERR_UNSUPPORTED),
+                       (dict(B=-1), H.ERR_INVALID_ARGUMENT), (dict(B=1 << 14, C=1 << 12), H.ERR_UNSUPPORTED),
                        (dict(B=1 << 62, C=1 << 62), H.ERR_UNSUPPORTED)):
         names, tail = kinds(**kw)[fn]
         assert call(fn, pointers(len(names)), tail) == status, kw
