@@ -43,7 +43,7 @@ __device__ __forceinline__ Span lane_span(const FwdTile<TS>& t, float (&e)[kScan
     const float s = decay(get(t.la, j));
     e[j] = pow2f(s);
     sp.u = advance(e[j], sp.u, input(t, j));
-    sp.s += s;
+    sp.s = join(sp.s, s);
   }
   return sp;
 }
@@ -54,6 +54,7 @@ template <typename TS, int G, int W, bool LINKED>
 __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) scan_forward(ScanArgs a) {
   __shared__ Span joint[2][W > 1 ? W : 1];
   const uint32_t group = LINKED ? link_row(a) : blockIdx.x, seg = LINKED ? link_draw(a, group) : 0;
+  if (LINKED && seg >= (uint32_t)a.nseg) return;
   const Place<G, W> at(a.R, group);
   const int64_t len = row_length(a, at.row), base = at.row * a.L;
   const float D = ld1(reinterpret_cast<const TS*>(a.D) + (uint32_t)at.row % (uint32_t)a.C);

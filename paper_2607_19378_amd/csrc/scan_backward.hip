@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256, LINKED ? 4 : 1) scan_gra
   __shared__ Span joint[2][W > 1 ? W : 1];
   __shared__ double sums[W];
   const uint32_t group = LINKED ? link_row(a) : blockIdx.x, turn = LINKED ? link_draw(a, group) : 0;
+  if (LINKED && turn >= (uint32_t)a.nseg) return;
   const uint32_t seg = LINKED ? a.nseg - 1 - turn : 0;
   const Place<G, W> at(a.R, group);
   const int64_t len = row_length(a, at.row), base = at.row * a.L;
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256, LINKED ? 4 : 1) scan_gra
       const float s = decay(get(cur.la, j));
       e[j] = pow2f(s);
       sp.u = advance(e[j], sp.u, input(cur, j));
-      sp.s += s;
+      sp.s = join(sp.s, s);
     }
     keep_packed(cur.x1);
     keep_packed(cur.v);

@@ -34,10 +34,17 @@ struct Span {
   float s, u;
 };
 
+// log2 of a product of two decays; a start in either one stays one, also beside a
+// NaN or a decay of infinity (whose NaN is in u, too)
+__device__ __forceinline__ float join(float a, float b) {
+  const float s = a + b;
+  return s == s ? s : fminf(a, b);
+}
+
 // first, then second
 __device__ __forceinline__ Span then(Span first, Span second) {
   const float r = fmaf(pow2f(second.s), first.u, second.u);
-  return {first.s + second.s, second.s == neg_inf() ? second.u : r};
+  return {join(first.s, second.s), second.s == neg_inf() ? second.u : r};
 }
 
 __device__ __forceinline__ float through(Span sp, float x) {
@@ -130,10 +137,14 @@ __device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
 // state behind it, and takes the spans between from there on in their order, so
 // that the roundings do not depend on the timing.  Each wait ends: a row's first
 // segment waits for nothing, and each other one for segments that are being worked on.
+// (Two calls at once on one workspace, which callers may not make, spoil the words: a
+// draw beyond the row's segments takes none, and a wait that lasts for seconds gives
+// up, with NaN.)
 //
 // Two words a segment, each written at once with its flag in the upper half:
 // word 0 (kSpan, s); word 1 (kSpan, u), later (kState, the state behind it).
 constexpr uint64_t kSpan = 1, kState = 2;
+constexpr int kMostPolls = 1 << 22;
 
 __device__ __forceinline__ uint64_t link_word(uint64_t flag, float x) { return flag << 32 | __float_as_uint(x); }
 __device__ __forceinline__ float link_value(uint64_t w) { return __uint_as_float((uint32_t)w); }
@@ -178,21 +189,29 @@ __device__ __forceinline__ float link_enter(uint64_t* row, uint32_t i, Span mine
     const bool there = (uint32_t)lane < i;
     const uint64_t* at = row + 2 * (there ? i - 1 - lane : 0);
     uint64_t w = 0;
-    int from;
-    for (;;) {
+    int from = -1;
+    for (int polls = 0; polls < kMostPolls; ++polls) {
       if (there && w >> 32 != kState) w = link_load(at + 1);
       const uint64_t done = __ballot(there && w >> 32 == kState), known = __ballot(there && w >> 32 != 0);
       if (done) {
-        from = __builtin_ctzll(done);
-        const uint64_t between = (uint64_t(1) << from) - 1;
-        if ((known & between) == between) break;
+        const int nearest = __builtin_ctzll(done);
+        const uint64_t between = (uint64_t(1) << nearest) - 1;
+        if ((known & between) == between) {
+          from = nearest;
+          break;
+        }
       }
       __builtin_amdgcn_s_sleep(4);
     }
     uint64_t ws = link_word(kSpan, 0.f);
-    if (lane < from)
-      for (ws = link_load(at); ws >> 32 != kSpan; ws = link_load(at)) __builtin_amdgcn_s_sleep(1);
-    x = read_lane(link_value(w), from);
+    if (lane < from) {
+      ws = link_load(at);
+      for (int polls = 0; ws >> 32 != kSpan && polls < kMostPolls; ++polls) {
+        __builtin_amdgcn_s_sleep(1);
+        ws = link_load(at);
+      }
+    }
+    x = from < 0 ? __builtin_nanf("") : read_lane(link_value(w), from < 0 ? 0 : from);
     const float a = pow2f(link_value(ws));
     const uint64_t starts = __ballot(link_value(ws) == neg_inf());
     for (int l = from - 1; l >= 0; --l) {

@@ -655,10 +655,12 @@ class _Call:
         import torch
         self._device = like.get_device()
         if stream is None:
-            stream = torch.cuda.current_stream(self._device)
+            handle = torch._C._cuda_getCurrentRawStream(self._device)  # current_stream() without its object
+        else:
+            handle = stream.cuda_stream
         self._fn = fn
-        self._args = args + (stream.cuda_stream,)
-        self._current = torch.cuda.current_device
+        self._args = args + (handle,)
+        self._current = torch._C._cuda_getDevice  # torch.cuda.current_device() once CUDA is initialised
         self._keep = (keep, stream)
 
     def __call__(self) -> None:

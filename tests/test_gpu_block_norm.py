@@ -319,3 +319,20 @@ def test_offsets_beyond_32_bits():
     torch.cuda.synchronize()
     for s, t in ((x_out, xt), (n, nt), (g[0], gt[0]), (g[1], gt[1])):
         assert torch.equal(s[:, :, P - 100001:], t)
+
+
+def test_samples_beyond_32_bits():
+    """A sample of less than 4 GB behind more than 2^31 elements: what it gives alone."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    B, C, P = 5, 512, (1 << 20) + 8
+    x = torch.randn(1, C, P, device="cuda", dtype=torch.bfloat16).expand(B, C, P).contiguous()
+    w = [torch.randn(C, device="cuda", dtype=torch.bfloat16) for _ in range(3)]
+    log("[norm] samples beyond 2^31 elements")
+    x_out, n = H.block_norm(x, x, x, *w)
+    g = H.block_norm_backward(x_out, x, x, *w, x, x)
+    torch.cuda.synchronize()
+    for t in (x_out, n) + g[:3]:
+        assert torch.equal(t[0], t[B - 1])
+    one = H.block_norm(x[:1].contiguous(), x[:1].contiguous(), x[:1].contiguous(), *w)
+    assert torch.equal(one[0][0], x_out[B - 1]) and torch.equal(one[1][0], n[B - 1])

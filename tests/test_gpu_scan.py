@@ -150,11 +150,17 @@ def test_starts_stop_infinities_and_nans():
             bad = x1.clone()
             bad[:, :, cut - 1] = float("inf")
             bad[0, :, 0] = float("nan")
-            yb, lastb, stb = H.scan(bad, *args[1:], return_last=True, return_states=True)
-            gb = H.scan_backward(bad, *args[1:], stb, gy)
+            wild = la.clone()  # and the decays themselves
+            wild[0, :, cut // 2] = float("nan")
+            wild[1, :, cut // 3] = float("inf")
+            yb, lastb, stb = H.scan(bad, x2, v, wild, D, return_last=True, return_states=True)
+            gb = H.scan_backward(bad, x2, v, wild, D, stb, gy)
             late = gy.clone()  # and nothing of the later sequence's gradient reaches the earlier one
             late[:, :, cut:] = float("nan")
-            gl = H.scan_backward(*args, st, late)
+            after = la.clone()
+            after[0, :, cut + 1:] = float("nan")
+            after[1, :, -1] = float("inf")
+            gl = H.scan_backward(x1, x2, v, after, D, st, late)
             torch.cuda.synchronize()
             assert torch.equal(yb[:, :, cut:], y[:, :, cut:]) and torch.equal(lastb, last)
             assert not torch.isfinite(yb[:, :, cut - 1]).any()
@@ -293,6 +299,59 @@ def test_views_at_any_alignment_and_nothing_behind_them():
             for (whole, t), want in zip(outs + grads, (y0, last0, st0) + g0):
                 assert torch.equal(t, want)
                 assert torch.all(whole[:3] == 7) and torch.all(whole[3 + t.numel():] == 7)
+
+
+def test_long_linked_rows_are_their_chunks():
+    """More segments than one look takes in, in both orders of the rows: what calls on 16384 positions at a time give,
+    whose states are handed on (fp32 roundings of the joins apart)."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    for R, L in ((2, 300001), (70, 300001)):
+        g = torch.Generator(device="cuda").manual_seed(R)
+        x1, x2, v, gy = (torch.randn(1, R, L, generator=g, device="cuda") for _ in range(4))
+        la = -0.002 * torch.rand(1, R, L, generator=g, device="cuda")
+        D, h0 = torch.randn(R, generator=g, device="cuda"), torch.randn(1, R, generator=g, device="cuda")
+        gh = torch.randn(1, R, generator=g, device="cuda")
+        log(f"[scan] linked rows {(R, L)}")
+        y, last, st = H.scan(x1, x2, v, la, D, h0=h0, return_last=True, return_states=True)
+        grads = H.scan_backward(x1, x2, v, la, D, st, gy, gh_last=gh, return_gh0=True)
+        h, parts = h0, []
+        for a in range(0, L, 16384):
+            cut = [t[:, :, a:a + 16384].contiguous() for t in (x1, x2, v, la)]
+            yc, h, sc = H.scan(*cut, D, h0=h, return_last=True, return_states=True)
+            parts.append((cut, yc, sc))
+        c, back = gh, []
+        for i, a in reversed(list(enumerate(range(0, L, 16384)))):
+            *gc, c = H.scan_backward(*parts[i][0], D, parts[i][2], gy[:, :, a:a + 16384].contiguous(), gh_last=c, return_gh0=True)
+            back.insert(0, gc)
+        torch.cuda.synchronize()
+        for got, want in [(y, torch.cat([p[1] for p in parts], 2)), (last, h), (grads[5], c)] + [
+                (grads[i], torch.cat([b[i] for b in back], 2)) for i in range(4)]:
+            assert float((got - want).norm() / want.norm()) < 2e-6  # some sixteen roundings of 2^-24 against each other
+
+
+def test_two_streams_at_once():
+    """Split calls that run at the same time, each on its own workspace."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    x1, x2, v, gy = (torch.randn(1, 40, 60000, device="cuda") for _ in range(4))
+    la, D = -torch.rand(1, 40, 60000, device="cuda") / 100, torch.randn(40, device="cuda")
+    want = H.scan(x1, x2, v, la, D, return_states=True)
+    gw = H.scan_backward(x1, x2, v, la, D, want[2], gy)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for _ in range(5):
+                f = H.scan(x1, x2, v, la, D, return_states=True)
+                b = H.scan_backward(x1, x2, v, la, D, f[2], gy)
+            got.append((f[0], f[2]) + b)
+    torch.cuda.synchronize()
+    for one in got:
+        for p, q in zip(one, (want[0], want[2]) + gw):
+            assert torch.equal(p, q)
 
 
 def test_captured_and_replayed():
