@@ -210,7 +210,7 @@ hipError_t forward(const NormArgs& a, const NormShape& s, hipStream_t st) {
 // where four would halve the width to 16 bytes (2 x 2048 x 2048 bf16: 30 against
 // 34 us; 2 x 512 x 8192: 27 against 21 us for 128 bytes in place of 64).  The backward
 // takes as few channels a thread as fit (2 x 512 x 8192 bf16: 50 us with two, 56 us
-// with four).
+// with four), and gives up tiles of 16 bytes for two sweeps (norm_sums).
 NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) {
   NormShape s;
   const int V = bf16 ? 8 : 4;
@@ -226,6 +226,7 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
   const int64_t groups = (P + s.V - 1) / s.V;
   int lp = 0;
   while (lp < 3 && (int64_t(1) << lp) < groups) ++lp;
+  const int widest = lp;
   // 32-bit offsets in a sample's tensors
   if (C * P <= (int64_t(1) << 32) / (bf16 ? 2 : 4) - 4096) {
     for (; lp >= 0; --lp) {
@@ -233,14 +234,16 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
         if (take(1, lp, kMaxNT) || take(4, lp, kMaxNT) || (!backward && take(8, lp, kMaxNT))) return s;
         continue;
       }
+      if (backward && lp == 0 && widest > 0) break;
       const bool many = (groups >> lp) * B >= 512;
       if (!backward && many && (take(1, lp, 512) || take(2, lp, 512) || take(4, lp, 512))) return s;
       if (take(1, lp, kMaxNT) || take(2, lp, kMaxNT) || take(4, lp, norm_threads(4))) return s;
       if (!backward && lp <= 1 && take(8, lp, norm_threads(8))) return s;
     }
   }
-  s.lp = 0;
+  s.lp = widest;
   s.K = 0;
+  if (!backward) s.lp = 0;
   s.NT = (int)(C < kMaxNT ? threads(1, 0) : kMaxNT);
   return s;
 }

@@ -27,17 +27,6 @@ struct BwdRow {
   Raw<TS, V> x, gn, gxo, z, g;
 };
 
-template <typename TS, int V>
-__device__ __forceinline__ void load_row(BwdRow<TS, V>& r, const NormArgs& a, int64_t o, int n) {
-  r.x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + o, n);
-  if (a.gn) r.gn = load<TS, V>(reinterpret_cast<const TS*>(a.gn) + o, n);
-  if (a.z) {
-    r.z = load<TS, V>(reinterpret_cast<const TS*>(a.z) + o, n);
-    if (a.g) r.g = load<TS, V>(reinterpret_cast<const TS*>(a.g) + o, n);
-  }
-  if (a.gx_out) r.gxo = load<TS, V>(reinterpret_cast<const TS*>(a.gx_out) + o, n);
-}
-
 // What is left of the sums of the first kind: q = 1 / rms(x), q^3 mean(gn w_pre x), r = 1 / rms(t)
 template <typename F>
 __device__ __forceinline__ float first_kind(const NormArgs& a, int m, F sum) {
@@ -284,62 +273,162 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
   }
 }
 
-// More channels than registers hold: the tile is read again for each sum, and
-// the weight sums are added up in the workspace, each by its own thread.
+// Where a tile of 32 bytes or more of a row does not fit in registers, the tensors
+// are read twice in place of once: norm_sums leaves each point's sums over a part of
+// the channels, norm_apply joins them and does the rest.  (2 x 2048 x 2048 bf16: 59 us
+// against 81 us for tiles of 16 bytes in registers; 2 x 1024 x 4095 bf16: 97 us against 74 us
+// for tiles of 32 bytes in registers, so only tiles of 16 bytes are given up.)  gmw is linear in gx_out, gn and
+// x, so its sum with t follows from three more sums of the first sweep:
+//   sum gmw t = sum w t gx_out + q sum w t gn w_pre - q^3 mean(gn w_pre x) sum w t x,
+// w = drop's factor w_post scale.
+constexpr int kSplitNT = 256;
+constexpr int kSums = 6;  // x x, gn w_pre x, t t, and w t with gx_out, gn w_pre, x
+
+// The raw inputs, t and w of V points of a channel
 template <typename TS, int V>
-__global__ void __launch_bounds__(kMaxNT) norm_backward_reread(NormArgs a) {
-  using Has = Parts<false, false, false, false>;
-  __shared__ Joint<3, V> lds;
-  __shared__ Joint<1, V> lds1;
+struct SplitRow {
+  BwdRow<TS, V> r;
+  float t[V], half[V];
+  uint32_t drawn[4];
+  float w_pre, wp;
+  __device__ __forceinline__ SplitRow(const NormArgs& a, const Draws& draws, int64_t b, int c, int64_t p, int n) {
+    const int64_t o = (b * a.C + c) * a.P + p;
+    r = BwdRow<TS, V>{};
+    r.x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + o, n);
+    w_pre = wp = 0.f;
+    if (a.gn) {
+      r.gn = load<TS, V>(reinterpret_cast<const TS*>(a.gn) + o, n);
+      w_pre = weight<TS>(a.w_pre, c);
+    }
+    if (a.gx_out) r.gxo = load<TS, V>(reinterpret_cast<const TS*>(a.gx_out) + o, n);
+    if (!a.z) return;
+    wp = weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) * a.kept;
+    r.z = load<TS, V>(reinterpret_cast<const TS*>(a.z) + o, n);
+    if (a.g) r.g = load<TS, V>(reinterpret_cast<const TS*>(a.g) + o, n);
+    if (a.drop) draws.words<V, false>(b * a.C + c, p, 0, drawn);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      half[j] = a.g ? gate(get(r.g, j)) : __uint_as_float(0x80000000u);
+      t[j] = get(r.z, j) * sigmoid_of(half[j]);
+    }
+  }
+};
+
+// A workgroup's part of the channels of a tile.
+struct Part {
+  uint32_t index;
+  int from, to;
+  __device__ __forceinline__ Part(const NormArgs& a, uint32_t i) {
+    index = i;
+    from = i * a.part;
+    to = from + a.part < a.C ? from + a.part : a.C;
+  }
+};
+
+template <typename TS, int V>
+__global__ void __launch_bounds__(kSplitNT) norm_sums(NormArgs a) {
+  __shared__ Joint<kSums, V> lds;
   const Draws draws(a);
-  float2* partial = a.partial + (int64_t)blockIdx.x * a.C;  // lp = 0: a channel is one thread's
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) partial[c] = make_float2(0.f, 0.f);
+  const int points = V << a.lp;
   for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
     const uint32_t tile = tile_of(a, turn);
     if (tile >= a.tiles) continue;
     const Spot<V> at(a, tile);
     const int n = clamp_count<V>(a.P - at.p);
-    auto where = [&](int c) { return (at.b * a.C + c) * a.P + at.p; };
-    BwdRow<TS, V> r;
-    float acc[3][V], sum[1][V], gx[V], gmw[V];
-    const Branch<V> branch(0);
+    const Part part(a, blockIdx.y);
+    float acc[kSums][V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = acc[2][j] = sum[0][j] = 0.f;
-    for (int c = at.cl; c < a.C; c += at.CL) {
-      load_row(r, a, where(c), n);
-      first_sums<Has>(r, a, a.gn ? weight<TS>(a.w_pre, c) : 0.f, branch, acc);
+    for (int m = 0; m < kSums; ++m)
+#pragma unroll
+      for (int j = 0; j < V; ++j) acc[m][j] = 0.f;
+    if (n > 0)
+      for (int c = part.from + at.cl; c < part.to; c += at.CL) {
+        const SplitRow<TS, V> s(a, draws, at.b, c, at.p, n);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float x = get(s.r.x, j), g = get(s.r.gn, j) * s.w_pre;
+          acc[0][j] = fmaf(x, x, acc[0][j]);
+          acc[1][j] = fmaf(g, x, acc[1][j]);
+          if (a.z) {
+            const float wt = !a.drop || draws.keeps(s.drawn, j) ? s.wp * s.t[j] : 0.f;
+            acc[2][j] = fmaf(s.t[j], s.t[j], acc[2][j]);
+            acc[3][j] = fmaf(wt, get(s.r.gxo, j), acc[3][j]);
+            acc[4][j] = fmaf(wt, g, acc[4][j]);
+            acc[5][j] = fmaf(wt, x, acc[5][j]);
+          }
+        }
+      }
+    over_channels(acc, lds, a.lp, at.pg, [](int m, auto sum, int) { return sum(m); });
+    float* to = a.sums + ((int64_t)tile * gridDim.y + part.index) * kSums * points;
+    for (int i = threadIdx.x; i < kSums * points; i += kSplitNT) to[i] = lds.all[i / points][i % points];
+    __syncthreads();  // read before the next tile's
+  }
+}
+
+template <typename TS, int V>
+__global__ void __launch_bounds__(kSplitNT) norm_apply(NormArgs a) {
+  __shared__ float sum[kSums][kMaxLanes * V];
+  // of each point: q, q^3 mean(gn w_pre x), r, r^3 mean(gmw t)
+  __shared__ float of[4][kMaxLanes * V];
+  const Draws draws(a);
+  const int points = V << a.lp;
+  float2* partial = a.partial + (int64_t)blockIdx.x * a.C;
+  const Part part(a, blockIdx.y);
+  // a channel's weight sums are kept by the first lane over its points
+  for (int c = part.from + (threadIdx.x >> a.lp); c < part.to; c += kSplitNT >> a.lp)
+    if ((threadIdx.x & ((1 << a.lp) - 1)) == 0) partial[c] = make_float2(0.f, 0.f);
+  for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
+    const uint32_t tile = tile_of(a, turn);
+    if (tile >= a.tiles) continue;
+    const Spot<V> at(a, tile);
+    const int n = clamp_count<V>(a.P - at.p);
+    const float* from = a.sums + (int64_t)tile * gridDim.y * kSums * points;
+    for (int i = threadIdx.x; i < kSums * points; i += kSplitNT) {
+      float x = 0.f;
+#pragma unroll 8
+      for (uint32_t k = 0; k < gridDim.y; ++k) x += from[(int64_t)k * kSums * points + i];
+      sum[i / points][i % points] = x;
     }
-    over_channels(acc, lds, a.lp, at.pg, [&](int m, auto sum, int) { return first_kind(a, m, sum); });
-    // the second sums of a channel, and with them all that its last row takes
-    auto row = [&](int c, float (&to)[1][V], float2* w) {
-      float none[3][V];
-      load_row(r, a, where(c), n);
-      const float w_pre = a.gn ? weight<TS>(a.w_pre, c) : 0.f, wp = a.z ? weight<TS>(a.w_post, c) * weight<TS>(a.scale, c) * a.kept : 0.f;
-#pragma unroll
-      for (int j = 0; j < V; ++j) none[0][j] = none[1][j] = none[2][j] = 0.f;
-      first_sums<Has>(r, a, w_pre, branch, none);
-      second_sums<Has>(r, a, draws, at.b * a.C + c, at.p, 0, w_pre, wp, lds, at.pg, branch, gx, gmw, to, w);
-    };
-    for (int c = at.cl; c < a.C; c += at.CL) {
+    __syncthreads();
+    if ((int)threadIdx.x < points) {
+      const int i = threadIdx.x;
+      const float C = (float)a.C, q = inverse_rms(sum[0][i], a.C, a.eps_pre), r = inverse_rms(sum[2][i], a.C, a.eps_post);
+      const float mean = a.gn ? sum[1][i] / C * q * q * q : 0.f;
+      of[0][i] = q;
+      of[1][i] = mean;
+      of[2][i] = r;
+      of[3][i] = (fmaf(q, sum[4][i], sum[3][i]) - mean * sum[5][i]) / C * r * r * r;
+    }
+    __syncthreads();
+    for (int c = part.from + at.cl; c < part.to; c += at.CL) {
+      const SplitRow<TS, V> s(a, draws, at.b, c, at.p, n);
+      float gx[V], gz[V], gg[V];
       float2 w = make_float2(0.f, 0.f);
-      row(c, sum, &w);
-      partial[c] = make_float2(partial[c].x + w.x, fmaf(w.y, a.kept, partial[c].y));
-      if (!a.z) store<TS, V>(reinterpret_cast<TS*>(a.gx) + where(c), gx, n);
-    }
-    if (!a.z) continue;
-    over_channels(sum, lds1, a.lp, at.pg, [&](int, auto sum, int point) { return second_kind(a, lds, point, sum(0)); });
-    for (int c = at.cl; c < a.C; c += at.CL) {
-      float unused[1][V];
-      float2 none = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int j = 0; j < V; ++j) unused[0][j] = 0.f;
-      row(c, unused, &none);
-      store<TS, V>(reinterpret_cast<TS*>(a.gx) + where(c), gx, n);
-      float gz[V], gg[V];
-      last_row<Has>(a, lds, lds1, at.pg, branch, gmw, gz, gg);
-      store<TS, V>(reinterpret_cast<TS*>(a.gz) + where(c), gz, n);
-      if (a.gg) store<TS, V>(reinterpret_cast<TS*>(a.gg) + where(c), gg, n);
+      for (int j = 0; j < V; ++j) {
+        const int i = at.pg * V + j;
+        const float q = of[0][i], r = of[2][i], x = get(s.r.x, j), gnq = get(s.r.gn, j) * q;
+        gx[j] = fmaf(-x, of[1][i], fmaf(gnq, s.w_pre, get(s.r.gxo, j)));
+        if (j < n) w.x = fmaf(gnq, x, w.x);
+        if (a.z) {
+          const float kept = !a.drop || draws.keeps(s.drawn, j) ? gx[j] : 0.f;
+          const float gt = fmaf(-s.t[j], of[3][i], r * (kept * s.wp));
+          if (j < n) w.y = fmaf(kept, s.t[j] * r, w.y);
+          gz[j] = gt * sigmoid_of(s.half[j]);
+          gg[j] = gt * s.t[j] * rest_of(s.half[j]);
+        }
+      }
+      const int64_t o = (at.b * a.C + c) * a.P + at.p;
+      store<TS, V>(reinterpret_cast<TS*>(a.gx) + o, gx, n);
+      if (a.z) store<TS, V>(reinterpret_cast<TS*>(a.gz) + o, gz, n);
+      if (a.g) store<TS, V>(reinterpret_cast<TS*>(a.gg) + o, gg, n);
+      for (int d = 1; d < (1 << a.lp); d *= 2) {
+        w.x += __shfl_xor(w.x, d);
+        w.y += __shfl_xor(w.y, d);
+      }
+      if (at.pg == 0) partial[c] = make_float2(partial[c].x + w.x, fmaf(w.y, a.kept, partial[c].y));
     }
+    __syncthreads();  // `of` is read before the next tile's
   }
 }
 
@@ -372,11 +461,21 @@ __global__ void __launch_bounds__(1024) norm_weights(NormArgs a) {
   }
 }
 
-// The workgroups that the chip holds at once (16 wavefronts a CU of the registers that
-// a tile takes): each goes through its share of the tiles.
-int groups_of(uint32_t turns, int NT) {
-  const uint32_t most = 256u * (NT >= 1024 ? 1 : 1024 / NT);
-  return (int)(turns < most ? turns : most);
+// The workgroups of the whole chip (16 wavefronts a CU of the registers that a tile takes):
+// each goes through its share of the tiles.  Of a split call at most 1024.
+int groups_of(const NormArgs& a, const NormShape& s) {
+  const uint32_t most = s.K == 0 ? 1024u : 256u * (s.NT >= 1024 ? 1 : 1024 / s.NT);
+  return (int)(a.turns < most ? a.turns : most);
+}
+
+// A split call's channels in parts: four workgroups a CU with those of all tiles, but few
+// enough that the joining of a tile's sums, which each of them does, stays small.
+void split_parts(NormArgs& a, const NormShape& s) {
+  const int CL = kSplitNT >> s.lp, rows = (a.C + CL - 1) / CL;
+  const uint32_t enough = (1024 + a.tiles - 1) / a.tiles, wanted = enough < 32 ? enough : 32;
+  const int parts = wanted < (uint32_t)rows ? (int)wanted : rows, each = (rows + parts - 1) / parts;
+  a.part = each * CL;
+  a.parts = (rows + each - 1) / each;
 }
 
 // A kernel's dynamic LDS limit is raised beyond the default 64 KB once.
@@ -416,19 +515,37 @@ hipError_t backward_parts(const NormArgs& a, const NormShape& s, hipStream_t st)
              : backward_held<TS, Parts<true, false, false, TAIL>>(a, s, st);
 }
 
+template <typename TS, int V>
+hipError_t backward_split(const NormArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)a.groups, (unsigned)a.parts);
+  hipLaunchKernelGGL((norm_sums<TS, V>), grid, dim3(kSplitNT), 0, st, a);
+  hipLaunchKernelGGL((norm_apply<TS, V>), grid, dim3(kSplitNT), 0, st, a);
+  return hipGetLastError();
+}
+
 template <typename TS>
 hipError_t backward(const NormArgs& a, const NormShape& s, hipStream_t st) {
-  constexpr int V = 16 / sizeof(TS);
-  const size_t lds = (size_t)2 * s.V * s.NT * sizeof(float);
   hipError_t err;
   if (s.K > 0)
     err = a.P % s.V == 0 ? backward_parts<TS, false>(a, s, st) : backward_parts<TS, true>(a, s, st);
   else
-    err = s.V == 1 ? launch<norm_backward_reread<TS, 1>>(a, s.NT, lds, st) : launch<norm_backward_reread<TS, V>>(a, s.NT, lds, st);
+    err = s.V == 1 ? backward_split<TS, 1>(a, st) : backward_split<TS, 16 / sizeof(TS)>(a, st);
   if (err != hipSuccess) return err;
   hipLaunchKernelGGL((norm_weights<TS>), dim3((unsigned)((a.C + 31) / 32)), dim3(1024), 0, st, a);
   return hipGetLastError();
 }
+
+// Everything of a call's shape.
+NormShape plan(NormArgs& a) {
+  const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, true);
+  norm_tiles(a, s);
+  a.groups = groups_of(a, s);
+  a.parts = 0;
+  if (s.K == 0) split_parts(a, s);
+  return s;
+}
+
+size_t partial_bytes(const NormArgs& a) { return (size_t)a.groups * (size_t)a.C * sizeof(float2); }
 
 }  // namespace
 
@@ -437,16 +554,15 @@ size_t norm_backward_workspace_bytes(int64_t B, int64_t C, int64_t P, bool bf16)
   a.B = B;
   a.C = (int)C;
   a.P = P;
-  const NormShape s = norm_shape(C, P, B, bf16, true);
-  norm_tiles(a, s);
-  return (size_t)groups_of(a.turns, s.NT) * (size_t)C * sizeof(float2);
+  a.bf16 = bf16;
+  const NormShape s = plan(a);
+  return partial_bytes(a) + (size_t)a.tiles * a.parts * kSums * ((size_t)s.V << s.lp) * sizeof(float);
 }
 
 hipError_t launch_norm_backward(const NormArgs& args, hipStream_t st) {
   NormArgs a = args;
-  const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, true);
-  norm_tiles(a, s);
-  a.groups = groups_of(a.turns, s.NT);
+  const NormShape s = plan(a);
+  a.sums = reinterpret_cast<float*>(reinterpret_cast<char*>(a.partial) + partial_bytes(a));
   return a.bf16 ? backward<uint16_t>(a, s, st) : backward<float>(a, s, st);
 }
 

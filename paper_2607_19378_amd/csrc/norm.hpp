@@ -26,7 +26,9 @@ struct NormArgs {
   uint32_t tiles, row_tiles;        // tiles of points in all, and of a sample
   uint32_t log_run;                 // log2 of the consecutive tiles of an XCD's turn
   uint32_t turns;                   // tiles, and the turns that fall behind the last one
-  int groups;                       // workgroups of the backward
+  int groups;                       // workgroups of the backward (of a part of the channels)
+  int part, parts;                  // split calls: channels of a part, and parts
+  float* sums;                      // [tiles, parts, sums of a point, points]
 };
 
 constexpr int64_t kMaxNormPoints = int64_t(1) << 33;  // B * P: tiles are counted in 32 bits
