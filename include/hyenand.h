@@ -449,7 +449,8 @@ hyenand_status hyenand_modal_filter(const float* log_mag, const float* angle, co
  *   positive one grows and overflows where the product of the decays of some
  *   span of positions does.  log_a below -87 (exp of it leaves fp32), -inf
  *   among it, starts a new sequence: h_t = u_t, whatever came before, an
- *   infinity or a NaN included.  Several sequences can so lie in one row.
+ *   infinity or a NaN included.  Several sequences can so lie in one row.  Behind
+ *   an infinity the state is an infinity or a NaN until the next start.
  * h0 (NULL: zeros), h_last (NULL: not written) : [B, C] fp32, the state before
  *   the first position and behind the last one.  h_last may be h0 itself.
  * lengths : [B] int64, or NULL for L everywhere.  Positions t >= lengths[b] are
@@ -459,7 +460,7 @@ hyenand_status hyenand_modal_filter(const float* log_mag, const float* angle, co
  * states : [B, C, ceil(L / HYENAND_SCAN_BLOCK)] fp32 or NULL: the state before
  *   every position that is a multiple of HYENAND_SCAN_BLOCK (behind the sample's
  *   end: its last one), which hyenand_scan_backward starts from.
- * B * C < 2^26, L <= 2^40, B * C * L <= 2^46.
+ * B * C <= 2^26 - 4, L <= 2^40, B * C * L <= 2^46.
  * workspace : at least hyenand_scan_workspace_size() bytes (0 for calls of many
  *   rows), 16-byte aligned; owned by the caller, its contents overwritten.
  * No output may overlap an input or another output, but for h_last = h0.
@@ -514,7 +515,7 @@ hyenand_status hyenand_scan_backward_workspace_size(int64_t B, int64_t C, int64_
  *   it touches no state and its y is 0.  Rows with the same slot are consecutive
  *   positions of one sequence, in the order of the batch.  States that no row
  *   names are left as they were.
- * B <= 65535, B * C < 2^26.  y and state overlap nothing.  No workspace.
+ * B <= 65535, B * C <= 2^26 - 4.  y and state overlap nothing.  No workspace.
  */
 hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, const void* log_a, const void* D,
                                  const int64_t* slots, float* state, void* y, int64_t B, int64_t C, int64_t num_slots,
@@ -534,6 +535,7 @@ hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, 
  *
  * with Sigmoid(x) = 1 / (1 + exp(-x)).  A point whose root is 0 (a point of zeros
  * without an eps) has the norm 0.  n is that of x_out before its rounding to dtype.
+ * Squares are fp32: magnitudes above 2^63 or, without an eps, below 2^-63 leave them.
  *
  * x, z, gate, x_out, n : contiguous [B, C, P] of dtype; w_post, scale, w_pre: [C]
  *   of dtype; all aligned to their element.  gate NULL: no gate.  scale NULL: 1.
@@ -550,7 +552,7 @@ hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, 
  *   easy as 1, 2, 3", 2011) with the 128-bit counter (r * ceil(P / 8) + i, offset)
  *   and the key seed, lower words first; a point is dropped where its half is
  *   below 65536 dropout_p.
- * B * C < 2^26, B * P <= 2^33.  No output may overlap an input or another
+ * B * C <= 2^26 - 4, B * P <= 2^33.  No output may overlap an input or another
  * output.  Compute is fp32; no workspace; validation, stream and error
  * conventions as for hyenand_fftconv; results are deterministic.
  */

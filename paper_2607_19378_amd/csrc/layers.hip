@@ -60,7 +60,7 @@ hyenand_status check_buffers(const Buffer (&b)[N], const char* same_out = "", co
   return HYENAND_OK;
 }
 
-constexpr int64_t kMaxRows = (int64_t(1) << 26) - 1;  // B * C: 64 work-items a row, fewer than 2^32 in a launch
+constexpr int64_t kMaxRows = (int64_t(1) << 26) - 4;  // B * C: 64 work-items a row, 4 rows a workgroup, fewer than 2^32 in a launch
 
 hyenand_status check_shape(int64_t B, int64_t C, int64_t L, const char* last, int dtype) {
   if (dtype != HYENAND_DTYPE_F32 && dtype != HYENAND_DTYPE_BF16)

@@ -191,14 +191,17 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256, LINKED ? 4 : 1) scan_gra
 template <typename TS>
 __global__ void __launch_bounds__(256) scan_sum_D(ScanArgs a) {
   __shared__ double part[4];
-  const uint32_t c = blockIdx.x, nseg = a.nseg, per = (uint32_t)a.R / a.C * nseg;
-  double x = 0.0;
+  const uint32_t nseg = a.nseg, per = (uint32_t)a.R / a.C * nseg;
+  for (int c = blockIdx.x; c < a.C; c += gridDim.x) {
+    double x = 0.0;
 #pragma unroll 4
-  for (uint32_t i = threadIdx.x; i < per; i += 256) x += a.partial[((int64_t)(i / nseg) * a.C + c) * nseg + i % nseg];
-  x = sum_lanes(x, 64);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  if (threadIdx.x == 0) st1(reinterpret_cast<TS*>(a.gD) + c, (float)(part[0] + part[1] + part[2] + part[3]));
+    for (uint32_t i = threadIdx.x; i < per; i += 256) x += a.partial[((int64_t)(i / nseg) * a.C + c) * nseg + i % nseg];
+    x = sum_lanes(x, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    if (threadIdx.x == 0) st1(reinterpret_cast<TS*>(a.gD) + c, (float)(part[0] + part[1] + part[2] + part[3]));
+    __syncthreads();  // read before the next channel's
+  }
 }
 
 template <typename TS, int W>
@@ -234,7 +237,8 @@ hipError_t gradients(const ScanArgs& a, const ScanShape& p, hipStream_t s) {
     default: err = p.waves == 1 ? gradient_rows<TS, 1>(a, s) : (p.waves == 4 ? gradient_rows<TS, 4>(a, s) : gradient_rows<TS, 8>(a, s));
   }
   if (err != hipSuccess || (a.R == a.C && a.nseg == 1)) return err;
-  hipLaunchKernelGGL((scan_sum_D<TS>), dim3((unsigned)a.C), dim3(256), 0, s, a);
+  const int most = 1 << 20;  // workgroups (fewer than 2^32 work-items)
+  hipLaunchKernelGGL((scan_sum_D<TS>), dim3((unsigned)(a.C < most ? a.C : most)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

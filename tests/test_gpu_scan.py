@@ -435,3 +435,22 @@ def test_offsets_beyond_32_bits():
     for i in range(4):
         a, b = g1[i][:, C - 1:, tail].float(), g2[i][:, :, tail].float()
         assert float((a - b).norm() / b.norm()) < 4e-3, i
+
+
+def test_many_channels():
+    """More channels than a launch has workgroups for, of one position and two samples: gD is a sum of two products."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    B, C = 2, (1 << 24) + 3
+    log("[scan] 2^24 channels")
+    x1, x2, v, la, gy = (torch.randn(B, C, 1, device="cuda") for _ in range(5))
+    D = torch.randn(C, device="cuda")
+    y, _, states = H.scan(x1, x2, v, la, D, return_states=True)
+    gx1, gx2, gv, gla, gD = H.scan_backward(x1, x2, v, la, D, states, gy)[:5]
+    u, gz = x1.double() * v, gy.double() * x2
+    # one product of three factors and a sum of two terms: four roundings of 2^-24 of the terms' magnitudes
+    for got, ref, mag in ((gD, (gz * u).sum((0, 2)), (gz * u).abs().sum((0, 2))),
+                          (gx1, gz * v * (1 + D.double()[:, None]), (gz * v).abs() * (1 + D.double().abs()[:, None])),
+                          (gx2, gy * u * (1 + D.double()[:, None]), (gy * u).abs() * (1 + D.double().abs()[:, None]))):
+        assert torch.all((got.double() - ref).abs() <= 6 * 2.0 ** -24 * mag + 1e-37)
+    assert torch.all(gla == 0)
