@@ -252,7 +252,7 @@ void norm_tiles(NormArgs& a, const NormShape& s) {
   const int64_t points = (int64_t)s.V << s.lp, row_tiles = (a.P + points - 1) / points;
   a.lp = s.lp;
   a.row_tiles = (uint32_t)row_tiles;
-  a.tiles = (uint32_t)(row_tiles * a.B);  // fewer than 2^31 + 2^22: kMaxNormPoints points, of which a tile has 4 or a row's
+  a.tiles = (uint32_t)(row_tiles * a.B);  // fewer than 2^31 + 2^26: kMaxNormPoints points, of which a tile has 4 or a row's
   a.log_run = 5 - s.lp;  // 32 lanes' points: 512 bytes
   const uint32_t round = 8u << a.log_run;
   a.turns = (a.tiles + round - 1) / round * round;

@@ -1213,6 +1213,6 @@ hyenand_status hyenand_modal_filter(const float* log_mag, const float* angle, co
   return HYENAND_OK;
 }
 
-int hyenand_version(void) { return 400; }
+int hyenand_version(void) { return 500; }
 
 }  // extern "C"
