@@ -211,6 +211,11 @@ hipError_t forward(const NormArgs& a, const NormShape& s, hipStream_t st) {
 // 34 us; 2 x 512 x 8192: 27 against 21 us for 128 bytes in place of 64).  The backward
 // takes as few channels a thread as fit (2 x 512 x 8192 bf16: 50 us with two, 56 us
 // with four), and gives up tiles of 16 bytes for two sweeps (norm_sums).
+// Rows shorter than a lane's 16 bytes are one point a lane; four channels a thread where
+// threads of one would fill the chip (2^19 of them; 4096 x 1024 x 1 bf16: forward 21 against 53
+// us, at 256 samples 5.8 against 4.7) or, backward, fill it twice (43 against 66 us, at 512
+// samples 15.0 against 14.2), as long as more than a wavefront is left of a tile (8192 x 64 x 3
+// fp32: 37 against 32 us, forward 11 against 15).
 NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) {
   NormShape s;
   const int V = bf16 ? 8 : 4;
@@ -231,6 +236,8 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
   if (C * P <= (int64_t(1) << 32) / (bf16 ? 2 : 4) - 4096) {
     for (; lp >= 0; --lp) {
       if (s.V == 1) {
+        const int64_t fill = threads(1, lp) < (backward ? 512 : 256) ? 0 : B * threads(1, lp) >> 19;
+        if (fill >= (backward ? 2 : 1) && take(4, lp, kMaxNT)) return s;
         if (take(1, lp, kMaxNT) || take(4, lp, kMaxNT) || (!backward && take(8, lp, kMaxNT))) return s;
         continue;
       }

@@ -112,7 +112,7 @@ def test_channels(C, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,C", [(1, 1), (5, 1024), (33, 1000), (3, 4096), (2, 16384), (2, 17000)])
+@pytest.mark.parametrize("B,C", [(1, 1), (5, 1024), (33, 1000), (3, 4096), (2, 16384), (2, 17000), (700, 1000), (1200, 900), (2100, 250)])
 def test_tokens(B, C, dtype):
     run_case(B, C, 1, dtype)
 
