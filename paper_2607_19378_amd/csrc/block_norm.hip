@@ -255,15 +255,20 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
   return s;
 }
 
-void norm_tiles(NormArgs& a, const NormShape& s) {
+void norm_tiles(NormArgs& a, const NormShape& s, bool backward) {
   const int64_t points = (int64_t)s.V << s.lp, row_tiles = (a.P + points - 1) / points;
   a.lp = s.lp;
   a.row_tiles = (uint32_t)row_tiles;
   a.tiles = (uint32_t)(row_tiles * a.B);  // fewer than 2^31 + 2^26: kMaxNormPoints points, of which a tile has 4 or a row's
   // 32 lanes' points, 512 bytes, but every XCD has a turn (1 x 2048 x 256 fp32: 12 against 17 us
-  // forward, 14 against 24 backward), and samples of one tile share no lines
-  a.log_run = row_tiles > 1 ? 5 - s.lp : 0;
-  while (a.log_run > 0 && a.tiles < 8u << a.log_run) --a.log_run;
+  // forward, 14 against 24 backward).  Samples of one tile share no lines; forward they stay
+  // together all the same, or each XCD fetches the weights (32 x 1024 x 1 bf16: 3.7 against
+  // 4.4 us), backward every workgroup less is one less to add up (64 x 6000 x 1 bf16: 16
+  // against 37 us).
+  const bool tokens = row_tiles == 1;
+  a.log_run = tokens && backward ? 0 : 5 - s.lp;
+  if (!tokens)
+    while (a.log_run > 0 && a.tiles < 8u << a.log_run) --a.log_run;
   const uint32_t round = a.log_run > 0 ? 8u << a.log_run : 1;
   a.turns = (a.tiles + round - 1) / round * round;
 }
@@ -271,7 +276,7 @@ void norm_tiles(NormArgs& a, const NormShape& s) {
 hipError_t launch_norm(const NormArgs& args, hipStream_t st) {
   NormArgs a = args;
   const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, false);
-  norm_tiles(a, s);
+  norm_tiles(a, s, false);
   return a.bf16 ? forward<uint16_t>(a, s, st) : forward<float>(a, s, st);
 }
 

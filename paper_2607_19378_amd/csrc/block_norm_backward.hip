@@ -538,7 +538,7 @@ hipError_t backward(const NormArgs& a, const NormShape& s, hipStream_t st) {
 // Everything of a call's shape.
 NormShape plan(NormArgs& a) {
   const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, true);
-  norm_tiles(a, s);
+  norm_tiles(a, s, true);
   a.groups = groups_of(a, s);
   a.parts = 0;
   if (s.K == 0) split_parts(a, s);
