@@ -1,8 +1,10 @@
-"""The GPU tests of the recurrence reach the plans that they are meant for: a rule that moves fails here,
+"""The GPU tests of the recurrence and the norms reach the plans that they are meant for: a rule that moves fails here,
 without a GPU."""
+import numpy as np
 import pytest
 
 import layer_plans as plans
+import layer_ref as R
 
 
 @pytest.mark.parametrize("shape,waves,split", plans.SCAN)
@@ -11,3 +13,29 @@ def test_recurrence(shape, waves, split):
     lanes, w, nseg = plans.scan_plan(B * C, L)
     assert (lanes, w, nseg > 1) == (64, waves, split)
     assert -(-L // 512) > w  # more than one turn of the wavefronts, or more than one segment
+
+
+@pytest.mark.parametrize("shape,dtype,forward,backward", plans.NORM)
+def test_norms(shape, dtype, forward, backward):
+    f, b = (plans.norm_plan(*shape, dtype, way) for way in (False, True))
+    assert (f[2], b[2]) == (forward, backward)
+    points = 8 if dtype == "bf16" else 4
+    assert f[0] == b[0] == (points if shape[2] >= points else 1)
+
+
+def test_norms_reach_every_kind():
+    """Channels a thread, points a lane, whole and ragged rows: all that a dense set of shapes asks for are listed."""
+    def kinds(shapes):
+        return {(dtype, way, p[0] > 1, p[2], p[0] > 1 and p[2] > 0 and s[2] % p[0] > 0)
+                for s, dtype in shapes for way in (False, True) for p in [plans.norm_plan(*s, dtype, way)]}
+
+    dense = [((B, C, P), dtype) for dtype in ("f32", "bf16") for B in (1, 64, 3000) for P in (1, 2, 3, 5, 7, 8, 9, 40, 513, 4096)
+             for C in [1, 9, 60] + [2 ** i + d for i in range(6, 15) for d in (-3, 0, 3)]]
+    mine = {k[1:] for k in kinds([(s, dtype) for s, dtype, _, _ in plans.NORM])}
+    assert {k[1:] for k in kinds(dense)} == mine
+
+
+def test_masks_of_whole_tensors():
+    """The masks in arrays are those of the reference, drawn one after another."""
+    for B, C, P in ((2, 3, 1), (1, 5, 7), (2, 2, 29)):
+        assert np.array_equal(plans.keep_factors(B, C, P, 0.3, -5, 1 << 40), R.keep_factors(B, C, P, 0.3, -5, 1 << 40))
