@@ -9,7 +9,10 @@
 //
 // Bound by HBM: five tensors read and three written.  The dropped points are drawn
 // again from the counter.  A workgroup takes tile after tile and adds its weight
-// sums up in registers; a second kernel adds those of the workgroups, in order.
+// sums up in registers, in fp32 over at most kSumTiles tiles; those of the next ones
+// are a row of their own, and a second kernel adds all rows in 64 bits, in order.  So
+// a weight's gradient carries the roundings of 64 tiles, whatever the number of points
+// (2^30 equal terms of a channel: exact, against 4e-4 off in one fp32 sum a workgroup).
 #include <mutex>
 
 #include "norm_device.hpp"
@@ -158,6 +161,8 @@ __device__ __forceinline__ float second_kind(const NormArgs& a, const Joint<3, V
   return sum / (float)a.C * r * r * r;
 }
 
+constexpr int kSumTiles = 64;
+
 template <typename TS, int V, int K, typename Has>
 __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backward(NormArgs a) {
   __shared__ Joint<3, V> lds;
@@ -219,57 +224,61 @@ __global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backwa
     fetch_branch(at);
     fetch_stream(at);
   }
-  while (tile < a.tiles) {
-    const Held<TS, V, Has::TAIL> at(a, tile);
-    float acc[3][V], sum[1][V], gmw[K][V];
+  for (int row = 0; row < a.rows; ++row) {
+    for (int left = kSumTiles; left > 0 && tile < a.tiles; --left) {
+      const Held<TS, V, Has::TAIL> at(a, tile);
+      float acc[3][V], sum[1][V], gmw[K][V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = acc[2][j] = sum[0][j] = 0.f;
+      for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = acc[2][j] = sum[0][j] = 0.f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) first_sums<Has>(r[k], a, w_pre[k], Branch<V>(k), acc);
+      for (int k = 0; k < K; ++k) first_sums<Has>(r[k], a, w_pre[k], Branch<V>(k), acc);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      keep_packed(r[k].x);
-      keep_packed(r[k].gn);
-      keep_packed(r[k].gxo);
-    }
-    // the next tile's inputs come as soon as this one's have been used
-    const uint32_t next = next_tile();
-    if (next < a.tiles) fetch_branch(Held<TS, V, Has::TAIL>(a, next));
-    over_channels(acc, lds, a.lp, at.pg, [&](int m, auto sum, int) { return first_kind(a, m, sum); });
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float gx[V];
-      second_sums<Has>(r[k], a, draws, at.b * a.C + first + k * CL, at.p, at.shift, w_pre[k], wp[k], lds, at.pg, Branch<V>(k),
-                       gx, gmw[k], sum, &weights[k]);
-      if (first + k * CL < a.C && at.any()) at.store(a.gx, k, gx);
-      next_channel();
-    }
-    if (next < a.tiles) fetch_stream(Held<TS, V, Has::TAIL>(a, next));
-    tile = next;
-    if (!Has::z(a)) continue;
-    over_channels(sum, lds1, a.lp, at.pg, [&](int, auto sum, int point) { return second_kind(a, lds, point, sum(0)); });
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float gz[V], gg[V];
-      last_row<Has>(a, lds, lds1, at.pg, Branch<V>(k), gmw[k], gz, gg);
-      // the next inputs are there by now, or else they would be waited for behind these
-      // stores, and with them
-      if (k == 0) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-      if (first + k * CL < a.C && at.any()) {
-        at.store(a.gz, k, gz);
-        if (Has::g(a)) at.store(a.gg, k, gg);
+      for (int k = 0; k < K; ++k) {
+        keep_packed(r[k].x);
+        keep_packed(r[k].gn);
+        keep_packed(r[k].gxo);
       }
-      next_channel();
-    }
-  }
+      // the next tile's inputs come as soon as this one's have been used
+      const uint32_t next = next_tile();
+      if (next < a.tiles) fetch_branch(Held<TS, V, Has::TAIL>(a, next));
+      over_channels(acc, lds, a.lp, at.pg, [&](int m, auto sum, int) { return first_kind(a, m, sum); });
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    for (int d = 1; d < (1 << a.lp); d *= 2) {
-      weights[k].x += __shfl_xor(weights[k].x, d);
-      weights[k].y += __shfl_xor(weights[k].y, d);
+      for (int k = 0; k < K; ++k) {
+        float gx[V];
+        second_sums<Has>(r[k], a, draws, at.b * a.C + first + k * CL, at.p, at.shift, w_pre[k], wp[k], lds, at.pg, Branch<V>(k),
+                         gx, gmw[k], sum, &weights[k]);
+        if (first + k * CL < a.C && at.any()) at.store(a.gx, k, gx);
+        next_channel();
+      }
+      if (next < a.tiles) fetch_stream(Held<TS, V, Has::TAIL>(a, next));
+      tile = next;
+      if (!Has::z(a)) continue;
+      over_channels(sum, lds1, a.lp, at.pg, [&](int, auto sum, int point) { return second_kind(a, lds, point, sum(0)); });
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float gz[V], gg[V];
+        last_row<Has>(a, lds, lds1, at.pg, Branch<V>(k), gmw[k], gz, gg);
+        // the next inputs are there by now, or else they would be waited for behind these
+        // stores, and with them
+        if (k == 0) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+        if (first + k * CL < a.C && at.any()) {
+          at.store(a.gz, k, gz);
+          if (Has::g(a)) at.store(a.gg, k, gg);
+        }
+        next_channel();
+      }
     }
-    const int c = first + k * CL;
-    if ((threadIdx.x & ((1 << a.lp) - 1)) == 0 && c < a.C) a.partial[(int64_t)blockIdx.x * a.C + c] = make_float2(weights[k].x, weights[k].y * a.kept);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      for (int d = 1; d < (1 << a.lp); d *= 2) {
+        weights[k].x += __shfl_xor(weights[k].x, d);
+        weights[k].y += __shfl_xor(weights[k].y, d);
+      }
+      const int c = first + k * CL;
+      if ((threadIdx.x & ((1 << a.lp) - 1)) == 0 && c < a.C)
+        a.partial[((int64_t)row * gridDim.x + blockIdx.x) * a.C + c] = make_float2(weights[k].x, weights[k].y * a.kept);
+      weights[k] = make_float2(0.f, 0.f);
+    }
   }
 }
 
@@ -372,68 +381,71 @@ __global__ void __launch_bounds__(kSplitNT) norm_apply(NormArgs a) {
   __shared__ float of[4][kMaxLanes * V];
   const Draws draws(a);
   const int points = V << a.lp;
-  float2* partial = a.partial + (int64_t)blockIdx.x * a.C;
   const Part part(a, blockIdx.y);
-  // a channel's weight sums are kept by the first lane over its points
-  for (int c = part.from + (threadIdx.x >> a.lp); c < part.to; c += kSplitNT >> a.lp)
-    if ((threadIdx.x & ((1 << a.lp) - 1)) == 0) partial[c] = make_float2(0.f, 0.f);
-  for (uint32_t turn = blockIdx.x; turn < a.turns; turn += gridDim.x) {
-    const uint32_t tile = tile_of(a, turn);
-    if (tile >= a.tiles) continue;
-    const Spot<V> at(a, tile);
-    const int n = clamp_count<V>(a.P - at.p);
-    const float* from = a.sums + (int64_t)tile * gridDim.y * kSums * points;
-    for (int i = threadIdx.x; i < kSums * points; i += kSplitNT) {
-      float x = 0.f;
+  uint32_t turn = blockIdx.x;
+  for (int row = 0; row < a.rows; ++row) {
+    float2* partial = a.partial + ((int64_t)row * gridDim.x + blockIdx.x) * a.C;
+    // a channel's weight sums are kept by the first lane over its points
+    for (int c = part.from + (threadIdx.x >> a.lp); c < part.to; c += kSplitNT >> a.lp)
+      if ((threadIdx.x & ((1 << a.lp) - 1)) == 0) partial[c] = make_float2(0.f, 0.f);
+    for (int left = kSumTiles; left > 0 && turn < a.turns; --left, turn += gridDim.x) {
+      const uint32_t tile = tile_of(a, turn);
+      if (tile >= a.tiles) continue;
+      const Spot<V> at(a, tile);
+      const int n = clamp_count<V>(a.P - at.p);
+      const float* from = a.sums + (int64_t)tile * gridDim.y * kSums * points;
+      for (int i = threadIdx.x; i < kSums * points; i += kSplitNT) {
+        float x = 0.f;
 #pragma unroll 8
-      for (uint32_t k = 0; k < gridDim.y; ++k) x += from[(int64_t)k * kSums * points + i];
-      sum[i / points][i % points] = x;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < points) {
-      const int i = threadIdx.x;
-      const float C = (float)a.C, q = inverse_rms(sum[0][i], a.C, a.eps_pre), r = inverse_rms(sum[2][i], a.C, a.eps_post);
-      const float mean = a.gn ? sum[1][i] / C * q * q * q : 0.f;
-      of[0][i] = q;
-      of[1][i] = mean;
-      of[2][i] = r;
-      of[3][i] = (fmaf(q, sum[4][i], sum[3][i]) - mean * sum[5][i]) / C * r * r * r;
-    }
-    __syncthreads();
-    for (int c = part.from + at.cl; c < part.to; c += at.CL) {
-      const SplitRow<TS, V> s(a, draws, at.b, c, at.p, n);
-      float gx[V], gz[V], gg[V];
-      float2 w = make_float2(0.f, 0.f);
+        for (uint32_t k = 0; k < gridDim.y; ++k) x += from[(int64_t)k * kSums * points + i];
+        sum[i / points][i % points] = x;
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < points) {
+        const int i = threadIdx.x;
+        const float C = (float)a.C, q = inverse_rms(sum[0][i], a.C, a.eps_pre), r = inverse_rms(sum[2][i], a.C, a.eps_post);
+        const float mean = a.gn ? sum[1][i] / C * q * q * q : 0.f;
+        of[0][i] = q;
+        of[1][i] = mean;
+        of[2][i] = r;
+        of[3][i] = (fmaf(q, sum[4][i], sum[3][i]) - mean * sum[5][i]) / C * r * r * r;
+      }
+      __syncthreads();
+      for (int c = part.from + at.cl; c < part.to; c += at.CL) {
+        const SplitRow<TS, V> s(a, draws, at.b, c, at.p, n);
+        float gx[V], gz[V], gg[V];
+        float2 w = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int i = at.pg * V + j;
-        const float q = of[0][i], r = of[2][i], x = get(s.r.x, j), gnq = get(s.r.gn, j) * q;
-        gx[j] = fmaf(-x, of[1][i], fmaf(gnq, s.w_pre, get(s.r.gxo, j)));
-        if (j < n) w.x = fmaf(gnq, x, w.x);
-        if (a.z) {
-          const float kept = !a.drop || draws.keeps(s.drawn, j) ? gx[j] : 0.f;
-          const float gt = fmaf(-s.t[j], of[3][i], r * (kept * s.wp));
-          if (j < n) w.y = fmaf(kept, s.t[j] * r, w.y);
-          gz[j] = gt * sigmoid_of(s.half[j]);
-          gg[j] = gt * s.t[j] * rest_of(s.half[j]);
+        for (int j = 0; j < V; ++j) {
+          const int i = at.pg * V + j;
+          const float q = of[0][i], r = of[2][i], x = get(s.r.x, j), gnq = get(s.r.gn, j) * q;
+          gx[j] = fmaf(-x, of[1][i], fmaf(gnq, s.w_pre, get(s.r.gxo, j)));
+          if (j < n) w.x = fmaf(gnq, x, w.x);
+          if (a.z) {
+            const float kept = !a.drop || draws.keeps(s.drawn, j) ? gx[j] : 0.f;
+            const float gt = fmaf(-s.t[j], of[3][i], r * (kept * s.wp));
+            if (j < n) w.y = fmaf(kept, s.t[j] * r, w.y);
+            gz[j] = gt * sigmoid_of(s.half[j]);
+            gg[j] = gt * s.t[j] * rest_of(s.half[j]);
+          }
         }
+        const int64_t o = (at.b * a.C + c) * a.P + at.p;
+        store<TS, V>(reinterpret_cast<TS*>(a.gx) + o, gx, n);
+        if (a.z) store<TS, V>(reinterpret_cast<TS*>(a.gz) + o, gz, n);
+        if (a.g) store<TS, V>(reinterpret_cast<TS*>(a.gg) + o, gg, n);
+        for (int d = 1; d < (1 << a.lp); d *= 2) {
+          w.x += __shfl_xor(w.x, d);
+          w.y += __shfl_xor(w.y, d);
+        }
+        if (at.pg == 0) partial[c] = make_float2(partial[c].x + w.x, fmaf(w.y, a.kept, partial[c].y));
       }
-      const int64_t o = (at.b * a.C + c) * a.P + at.p;
-      store<TS, V>(reinterpret_cast<TS*>(a.gx) + o, gx, n);
-      if (a.z) store<TS, V>(reinterpret_cast<TS*>(a.gz) + o, gz, n);
-      if (a.g) store<TS, V>(reinterpret_cast<TS*>(a.gg) + o, gg, n);
-      for (int d = 1; d < (1 << a.lp); d *= 2) {
-        w.x += __shfl_xor(w.x, d);
-        w.y += __shfl_xor(w.y, d);
-      }
-      if (at.pg == 0) partial[c] = make_float2(partial[c].x + w.x, fmaf(w.y, a.kept, partial[c].y));
+      __syncthreads();  // `of` is read before the next tile's
     }
-    __syncthreads();  // `of` is read before the next tile's
   }
 }
 
-// The weights' gradients: the workgroups' sums, 32 channels a workgroup, every
-// 32nd of them a thread.
+// The weights' gradients: the rows' sums, 32 channels a workgroup, every 32nd row a
+// thread.
 template <typename TS>
 __global__ void __launch_bounds__(1024) norm_weights(NormArgs a) {
   __shared__ double sx[32][33], sy[32][33];
@@ -442,7 +454,7 @@ __global__ void __launch_bounds__(1024) norm_weights(NormArgs a) {
   double x = 0.0, y = 0.0;
   if (c < a.C)
 #pragma unroll 8
-    for (int i = part; i < a.groups; i += 32) {
+    for (int i = part; i < a.groups * a.rows; i += 32) {  // (fewer than 2^26)
       const float2 w = a.partial[(int64_t)i * a.C + c];
       x += w.x;
       y += w.y;
@@ -540,12 +552,14 @@ NormShape plan(NormArgs& a) {
   const NormShape s = norm_shape(a.C, a.P, a.B, a.bf16, true);
   norm_tiles(a, s, true);
   a.groups = groups_of(a, s);
+  const uint32_t each = (a.turns + a.groups - 1) / a.groups;
+  a.rows = (int)((each + kSumTiles - 1) / kSumTiles);
   a.parts = 0;
   if (s.K == 0) split_parts(a, s);
   return s;
 }
 
-size_t partial_bytes(const NormArgs& a) { return (size_t)a.groups * (size_t)a.C * sizeof(float2); }
+size_t partial_bytes(const NormArgs& a) { return (size_t)a.groups * (size_t)a.rows * (size_t)a.C * sizeof(float2); }
 
 }  // namespace
 

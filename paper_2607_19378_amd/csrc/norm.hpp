@@ -20,13 +20,13 @@ struct NormArgs {
   // backward: null where there is none
   const void *gx_out, *gn;
   void *gx, *gz, *gg, *gw_post, *gscale, *gw_pre;
-  float2* partial;                  // [groups, C] a workgroup's sums for the weights
+  float2* partial;                  // [rows, groups, C] a workgroup's sums for the weights, of 64 tiles a row
   // set by the launchers
   int lp;                           // log2 of the lanes over a channel's positions
   uint32_t tiles, row_tiles;        // tiles of points in all, and of a sample
   uint32_t log_run;                 // log2 of the consecutive tiles of an XCD's turn
   uint32_t turns;                   // tiles, and the turns that fall behind the last one
-  int groups;                       // workgroups of the backward (of a part of the channels)
+  int groups, rows;                 // workgroups of the backward (of a part of the channels), and rows of their sums
   int part, parts;                  // split calls: channels of a part, and parts
   float* sums;                      // [tiles, parts, sums of a point, points]
 };

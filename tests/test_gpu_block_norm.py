@@ -346,3 +346,22 @@ def test_samples_beyond_32_bits():
         assert torch.equal(t[0], t[B - 1])
     one = H.block_norm(x[:1].contiguous(), x[:1].contiguous(), x[:1].contiguous(), *w)
     assert torch.equal(one[0][0], x_out[B - 1]) and torch.equal(one[1][0], n[B - 1])
+
+
+@pytest.mark.parametrize("B,P", [((1 << 26) - 4, 1), (1, 1 << 29), (1, 1 << 30)])
+def test_weights_of_very_many_points(B, P):
+    """One channel, every point's term of each weight's gradient 1 + 2^-11, in tiles of one point, tiles in registers and
+    two sweeps.  The sum goes through fp32 over 64 tiles of 4 points (half a step each) at most, then through 64 bits."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    one, term = 1.0, 1 + 2.0 ** -11
+    x = torch.full((B, 1, P), one, device="cuda")
+    g = torch.full((B, 1, P), term, device="cuda")
+    w = torch.ones(1, device="cuda")
+    log(f"[norm] weights of {B} x {P} points")
+    # a single channel's norms are signs: gx = gx_out, and all three sums are those of the terms
+    grads = H.block_norm_backward(x, x, None, w, w, w, g, g, 0.0, 0.0)
+    torch.cuda.synchronize()
+    ref = term * B * P
+    for t in grads[3:]:
+        assert abs(float(t) - ref) <= (64 * 4 + 1) * 2.0 ** -24 * ref, float(t) / ref - 1
