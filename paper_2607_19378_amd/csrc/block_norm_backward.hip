@@ -303,9 +303,9 @@ struct SplitRow {
   __device__ __forceinline__ SplitRow(const NormArgs& a, const Draws& draws, int64_t b, int c, int64_t p, int n) {
     const int64_t o = (b * a.C + c) * a.P + p;
     r = BwdRow<TS, V>{};
-    r.x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + o, n);
     w_pre = wp = 0.f;
-    if (a.gn) {
+    if (a.gn) {  // without it x has no part in anything, be it an infinity or a NaN
+      r.x = load<TS, V>(reinterpret_cast<const TS*>(a.x) + o, n);
       r.gn = load<TS, V>(reinterpret_cast<const TS*>(a.gn) + o, n);
       w_pre = weight<TS>(a.w_pre, c);
     }

@@ -365,3 +365,20 @@ def test_weights_of_very_many_points(B, P):
     ref = term * B * P
     for t in grads[3:]:
         assert abs(float(t) - ref) <= (64 * 4 + 1) * 2.0 ** -24 * ref, float(t) / ref - 1
+
+
+@pytest.mark.parametrize("C,P", [(100, 33), (24, 1), (5000, 9), (17000, 1)])
+def test_stream_without_its_norm(C, P):
+    """Without gn the gradients do not depend on x_out, whatever stands there."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    x, z, gate, g = (torch.randn(2, C, P, device="cuda") for _ in range(4))
+    w, s = torch.randn(C, device="cuda"), torch.randn(C, device="cuda")
+    wild = x.clone()
+    wild[0, 1], wild[1, 2], wild[1, 3] = float("inf"), float("nan"), 3e38
+    want = H.block_norm_backward(x, z, gate, w, s, None, g, None)
+    got = H.block_norm_backward(wild, z, gate, w, s, None, g, None)
+    torch.cuda.synchronize()
+    assert torch.equal(want[0], g)
+    for name, a, b in zip(("gx", "gz", "ggate", "gw_post", "gscale"), got, want):
+        assert torch.isfinite(b).all() and torch.equal(a, b), name
