@@ -47,8 +47,10 @@ struct Branch {
   static constexpr int kWords = 2 * V;     // of a channel and thread
   float* at;
   __device__ __forceinline__ explicit Branch(int k) : at(branch_lds + ((size_t)k * kWords * blockDim.x + N * threadIdx.x)) {}
-  __device__ __forceinline__ void write(int what, int from, const float (&x)[N]) const { __builtin_memcpy(place(what, from), x, sizeof x); }
-  __device__ __forceinline__ void read(int what, int from, float (&x)[N]) const { __builtin_memcpy(x, place(what, from), sizeof x); }
+  template <typename T>
+  __device__ __forceinline__ void write(int what, int from, const T (&x)[N]) const { __builtin_memcpy(place(what, from), x, sizeof x); }
+  template <typename T>
+  __device__ __forceinline__ void read(int what, int from, T (&x)[N]) const { __builtin_memcpy(x, place(what, from), sizeof x); }
   __device__ __forceinline__ float* place(int what, int from) const {
     return reinterpret_cast<float*>(__builtin_assume_aligned(at + (size_t)(what * V + from) * blockDim.x, N * 4));
   }
@@ -63,7 +65,8 @@ __device__ __forceinline__ void first_sums(const BwdRow<TS, V>& r, const NormArg
   constexpr int N = Branch<V>::N;
 #pragma unroll
   for (int from = 0; from < V; from += N) {
-    float half[N], t[N];
+    float t[N];
+    uint32_t half[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int j = from + i;
@@ -138,7 +141,8 @@ __device__ __forceinline__ void last_row(const NormArgs& a, const Joint<3, V>& l
   constexpr int N = Branch<V>::N;
 #pragma unroll
   for (int from = 0; from < V; from += N) {
-    float rinv[N], mean[N], half[N], t[N];
+    float rinv[N], mean[N], t[N];
+    uint32_t half[N];
     branch.read(kT, from, t);
     if (Has::g(a)) branch.read(kGate, from, half);
     read_sums(lds, 2, pg, rinv, from);
@@ -297,8 +301,8 @@ constexpr int kSums = 6;  // x x, gn w_pre x, t t, and w t with gx_out, gn w_pre
 template <typename TS, int V>
 struct SplitRow {
   BwdRow<TS, V> r;
-  float t[V], half[V];
-  uint32_t drawn[4];
+  float t[V];
+  uint32_t half[V], drawn[4];
   float w_pre, wp;
   __device__ __forceinline__ SplitRow(const NormArgs& a, const Draws& draws, int64_t b, int c, int64_t p, int n) {
     const int64_t o = (b * a.C + c) * a.P + p;
@@ -317,7 +321,7 @@ struct SplitRow {
     if (a.drop) draws.words<V, false>(b * a.C + c, p, 0, drawn);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      half[j] = a.g ? gate(get(r.g, j)) : __uint_as_float(0x80000000u);
+      half[j] = a.g ? gate(get(r.g, j)) : kNoGate;
       t[j] = get(r.z, j) * sigmoid_of(half[j]);
     }
   }

@@ -19,15 +19,18 @@ using rows::Raw;
 constexpr int kMaxNT = 1024;
 constexpr int kMaxLanes = 8;  // over a channel's points
 
-// sigmoid(g) as the smaller of it and 1 - sigmoid(g), with the sign bit set where
-// that is the latter: both follow from it to an fp32 rounding of their own.
-__device__ __forceinline__ float gate(float g) {
+// sigmoid(g) as the bits of the smaller of it and 1 - sigmoid(g), with the sign bit
+// set where that is the latter: both follow from it to an fp32 rounding of their own.
+// Bits and no float: the smaller one is 0 for gates far from 0, and the library is
+// compiled with -fno-signed-zeros, which lets the sign of a float 0 be lost.
+__device__ __forceinline__ uint32_t gate(float g) {
   const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(g));
   const float m = e * __builtin_amdgcn_rcpf(1.f + e);
-  return __uint_as_float(__float_as_uint(m) | (~__float_as_uint(g) & 0x80000000u));
+  return __float_as_uint(m) | (~__float_as_uint(g) & 0x80000000u);
 }
-__device__ __forceinline__ float sigmoid_of(float m) { return __float_as_int(m) < 0 ? 1.f + m : m; }
-__device__ __forceinline__ float rest_of(float m) { return __float_as_int(m) < 0 ? -m : 1.f - m; }
+constexpr uint32_t kNoGate = 0x80000000u;  // of sigmoid 1
+__device__ __forceinline__ float sigmoid_of(uint32_t m) { return m >> 31 ? 1.f + __uint_as_float(m) : __uint_as_float(m); }
+__device__ __forceinline__ float rest_of(uint32_t m) { return m >> 31 ? -__uint_as_float(m) : 1.f - __uint_as_float(m); }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as
 // 1, 2, 3", 2011): four 32-bit words from a 128-bit counter and a 64-bit key.

@@ -382,3 +382,27 @@ def test_stream_without_its_norm(C, P):
     assert torch.equal(want[0], g)
     for name, a, b in zip(("gx", "gz", "ggate", "gw_post", "gscale"), got, want):
         assert torch.isfinite(b).all() and torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,P", [(8, 1), (8, 20), (200, 77), (5000, 9), (17000, 1)])
+def test_gates_whose_smaller_part_is_zero(C, P, dtype):
+    """Gates of 100 and more (sigmoid 1, its rest 0) are none, gates of -100 and less close the branch, and an absent gate
+    is an open one: forward and backward, bit for bit."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    x, z, a, b = (torch.randn(2, C, P, device="cuda").to(dt) for _ in range(4))
+    w = [torch.randn(C, device="cuda").to(dt) for _ in range(3)]
+    gate = torch.full((2, C, P), 200.0, device="cuda", dtype=dt)
+    gate[:, ::3], gate[:, 1::3] = 100.0, float("inf")
+    closed = gate.clone()
+    closed[:, 2::4], closed[:, 3::8] = -200.0, -float("inf")
+    for g, zz in ((gate, z), (closed, torch.where(closed > 0, z, 0.0))):
+        got, want = H.block_norm(x, z, g, *w), H.block_norm(x, zz, None, *w)
+        gg, gw = H.block_norm_backward(got[0], z, g, *w, a, b), H.block_norm_backward(want[0], zz, None, *w, a, b)
+        torch.cuda.synchronize()
+        for s, t in list(zip(got, want)) + [(gg[0], gw[0])] + list(zip(gg[3:], gw[3:])):
+            assert torch.equal(s, t)
+        assert torch.equal(gg[1], torch.where(g > 0, gw[1], 0.0)) and torch.all(gg[2] == 0)
+        assert torch.all(zz[:, 0] == z[:, 0]) and bool((gw[1] != 0).any())
