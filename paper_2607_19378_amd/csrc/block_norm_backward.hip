@@ -13,8 +13,6 @@
 // are a row of their own, and a second kernel adds all rows in 64 bits, in order.  So
 // a weight's gradient carries the roundings of 64 tiles, whatever the number of points
 // (2^30 equal terms of a channel: exact, against 4e-4 off in one fp32 sum a workgroup).
-#include <mutex>
-
 #include "norm_device.hpp"
 
 namespace hyenand {
@@ -494,15 +492,10 @@ void split_parts(NormArgs& a, const NormShape& s) {
   a.parts = (rows + each - 1) / each;
 }
 
-// A kernel's dynamic LDS limit is raised beyond the default 64 KB once.
 template <auto Kernel>
 hipError_t launch(const NormArgs& a, int NT, size_t lds, hipStream_t st) {
-  static std::once_flag once;
-  static hipError_t attr = hipSuccess;
-  std::call_once(once, [] {
-    attr = hipFuncSetAttribute(reinterpret_cast<const void*>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
-  });
-  if (attr != hipSuccess) return attr;
+  const hipError_t e = raise_lds_limit<Kernel>(128 * 1024);
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(Kernel, dim3((unsigned)a.groups), dim3((unsigned)NT), lds, st, a);
   return hipGetLastError();
 }

@@ -45,7 +45,6 @@
 #include <stdlib.h>
 #include <string.h>
 
-#include <mutex>
 
 #include "kernels.hpp"
 
@@ -964,13 +963,8 @@ hipError_t launch_mixed_t(const FftConvArgs& a, const MrPlan& pl, hipStream_t s)
   const size_t lds = mr_lds_bytes(pl, pl.Q);
   const unsigned nblk = (unsigned)((a.lines + 2 * pl.Q - 1) / (2 * pl.Q));
   // the kernel may take more than the default 64 KB of dynamic LDS
-  static std::once_flag once;
-  static hipError_t attr = hipSuccess;
-  std::call_once(once, [] {
-    attr = hipFuncSetAttribute(reinterpret_cast<const void*>(conv_mixed<TS, ACT, NT, FAM>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMrMaxLds);
-  });
-  if (attr != hipSuccess) return attr;
+  const hipError_t e = raise_lds_limit<conv_mixed<TS, ACT, NT, FAM>>(kMrMaxLds);
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL((conv_mixed<TS, ACT, NT, FAM>), dim3(nblk), dim3(NT), lds, s, (const TS*)a.x1, (const TS*)a.x2,
                      (const TS*)a.v, (const TS*)a.k, (const TS*)a.D, (TS*)a.y, (int)a.lines, (int)a.C, a.kC,
                      a.act_in, pl);
@@ -1031,13 +1025,8 @@ hipError_t launch_mixed_bwd_t(const FftConvBwdArgs& b, const MrPlan& pl, hipStre
   const FftConvArgs& a = b.f;
   const size_t lds = mr_lds_bytes_bwd(pl, pl.Q);
   const unsigned nblk = (unsigned)((a.lines + 2 * pl.Q - 1) / (2 * pl.Q));
-  static std::once_flag once;
-  static hipError_t attr = hipSuccess;
-  std::call_once(once, [] {
-    attr = hipFuncSetAttribute(reinterpret_cast<const void*>(conv_mixed_bwd<TS, NT, FAM>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMrMaxLds);
-  });
-  if (attr != hipSuccess) return attr;
+  const hipError_t e = raise_lds_limit<conv_mixed_bwd<TS, NT, FAM>>(kMrMaxLds);
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL((conv_mixed_bwd<TS, NT, FAM>), dim3(nblk), dim3(NT), lds, s, (const TS*)a.x1, (const TS*)a.x2,
                      (const TS*)a.v, (const TS*)a.k, (const TS*)a.D, (const TS*)b.gy, (TS*)b.gx1, (TS*)b.gx2,
                      (TS*)b.gv, (TS*)b.gk, b.partial, (int)a.lines, (int)a.C, pl);

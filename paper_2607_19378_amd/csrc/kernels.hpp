@@ -5,6 +5,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "device_once.hpp"
 #include "fft_device.hpp"
 
 namespace hyenand {
@@ -48,6 +49,19 @@ struct FftConvArgs {
 // before a call, so that the hipGetLastError after each of the call's
 // launches reports that launch only.
 inline void clear_pending_error() { (void)hipGetLastError(); }
+
+// Lets Kernel take up to `bytes` of dynamic LDS, beyond the default 64 KB, on the
+// current device: the attribute belongs to a kernel on one device.
+template <auto Kernel>
+hipError_t raise_lds_limit(size_t bytes) {
+  static DeviceOnce raised;
+  int device = 0;
+  const hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  return raised(device, [bytes] {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  });
+}
 
 // single pass (the padded problem of one line fits in LDS)
 bool fused1d_supported(int64_t P);

@@ -27,7 +27,6 @@
 // lane's own register quads, and the weights sit in LDS as bf16 in that
 // order, eight per 16-byte read.
 #include <algorithm>
-#include <mutex>
 
 #include "kernels.hpp"
 
@@ -430,18 +429,12 @@ size_t lds_floats(const SynthArgs& a, bool resident, bool bf) {
 
 constexpr size_t kLdsLimit = 160 * 1024;
 
-// one launch; the kernel's dynamic LDS limit is raised to the CU's 160 KB
-// once per kernel
-template <typename K>
-hipError_t launch_one(K kernel, int64_t grid, dim3 block, size_t bytes, hipStream_t s, const SynthArgs& a) {
-  static std::once_flag once;
-  static hipError_t attr = hipSuccess;
-  std::call_once(once, [&] {
-    attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               (int)kLdsLimit);
-  });
-  if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), block, bytes, s, a);
+// one launch; the kernel may take the CU's 160 KB of LDS
+template <auto Kernel>
+hipError_t launch_one(int64_t grid, dim3 block, size_t bytes, hipStream_t s, const SynthArgs& a) {
+  const hipError_t e = raise_lds_limit<Kernel>(kLdsLimit);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(Kernel, dim3((unsigned)grid), block, bytes, s, a);
   return hipGetLastError();
 }
 
@@ -469,9 +462,9 @@ hipError_t launch_film(SynthArgs a, hipStream_t s) {
   const int64_t grid = std::min<int64_t>(groups, (int64_t)ncu * std::min(per_cu, 2));
   const dim3 block(64 * kSynthWaves);
   switch (a.hidden) {
-    case 32: return launch_one(siren_synth<32, FILM, TS, BF>, grid, block, bytes, s, a);
-    case 64: return launch_one(siren_synth<64, FILM, TS, BF>, grid, block, bytes, s, a);
-    case 128: return launch_one(siren_synth<128, FILM, TS, BF>, grid, block, bytes, s, a);
+    case 32: return launch_one<siren_synth<32, FILM, TS, BF>>(grid, block, bytes, s, a);
+    case 64: return launch_one<siren_synth<64, FILM, TS, BF>>(grid, block, bytes, s, a);
+    case 128: return launch_one<siren_synth<128, FILM, TS, BF>>(grid, block, bytes, s, a);
     default: return hipErrorInvalidValue;
   }
 }
