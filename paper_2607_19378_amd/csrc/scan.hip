@@ -230,9 +230,12 @@ ScanShape scan_shape(int64_t R, int64_t L) {
     return p;
   }
   if (tiles > 1 && R < 4096) p.waves = R < 1024 && tiles > 4 ? 8 : 4;
-  if (R < 192 && tiles > 32 && R * tiles < (int64_t(1) << 24)) {  // (fewer than 2^32 work-items)
+  // A launch has fewer than 2^32 work-items: segments of 2^35 positions in all, more than five tensors in a
+  // card's memory.  (One row of 2^33, bf16, forward: 135 ms, against 3640 for one workgroup.)
+  const int64_t nseg = (tiles + kLinkedWaves - 1) / kLinkedWaves;
+  if (R < 192 && tiles > 32 && nseg <= ((int64_t(1) << 32) - 1) / (64 * kLinkedWaves) / R) {
     p.waves = kLinkedWaves;
-    p.nseg = (int)((tiles + kLinkedWaves - 1) / kLinkedWaves);
+    p.nseg = (int)nseg;
   }
   return p;
 }

@@ -454,3 +454,38 @@ def test_many_channels():
                           (gx2, gy * u * (1 + D.double()[:, None]), (gy * u).abs() * (1 + D.double().abs()[:, None]))):
         assert torch.all((got.double() - ref).abs() <= 6 * 2.0 ** -24 * mag + 1e-37)
     assert torch.all(gla == 0)
+
+
+def test_one_row_of_very_many_segments():
+    """A row of 2^33 positions: what its parts give from the states kept before them, and a sum over the whole of it."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    L, part, edge = (1 << 33) + 4099, 1 << 17, 1 << 14
+    if torch.cuda.mem_get_info()[0] < 160e9:
+        pytest.skip("needs 160 GB of GPU memory")
+    log("[scan] a row of 2^33 positions")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(1, 1, L, generator=g, device="cuda", dtype=torch.bfloat16)
+    la, D = torch.full_like(x, -0.01), torch.ones(1, device="cuda", dtype=torch.bfloat16)
+    y, last, st = H.scan(x, x, x, la, D, return_last=True, return_states=True)
+    grads = H.scan_backward(x, x, x, la, D, st, x)
+    torch.cuda.synchronize()
+    total = sum(float(x[..., i:i + (1 << 28)].double().pow(4).sum()) for i in range(0, L, 1 << 28))
+    # x2 is x and gy is x: gz u = x^4; half a step of bf16, and eight products and sums a lane before 64 bits
+    assert abs(float(grads[4]) - total) <= (2.0 ** -8 + 16 * 2.0 ** -24) * total
+    for a in (0, 1 << 20, 1 << 31, (1 << 32) - (1 << 16), (1 << 33) - (1 << 18), L - part):
+        a = a // 512 * 512
+        cut = slice(a, L if L - a < part + 512 else a + part)  # the last one to the end
+        one, decay = x[..., cut].contiguous(), la[..., cut].contiguous()
+        yc, lc, sc = H.scan(one, one, one, decay, D, h0=st[..., a // 512].contiguous(), return_last=True, return_states=True)
+        gc = H.scan_backward(one, one, one, decay, D, sc, one)
+        torch.cuda.synchronize()
+        # the part's sums are joined elsewhere: fp32 roundings, and a step of bf16 where they cross a border
+        assert torch.allclose(sc, st[..., a // 512:a // 512 + sc.shape[-1]], rtol=1e-4, atol=1e-4)
+        assert float((yc.float() - y[..., cut].float()).norm() / yc.float().norm()) < 4e-3
+        # what comes from behind the part has decayed by exp(-163) before its last 2^14 positions
+        inner = slice(0, one.shape[-1] if cut.stop == L else one.shape[-1] - edge)
+        for p, q in zip(gc[:4], grads[:4]):
+            p, q = p[..., inner].float(), q[..., cut][..., inner].float()
+            assert float((p - q).norm() / p.norm()) < 4e-3
+    assert torch.allclose(last, lc, rtol=1e-4)

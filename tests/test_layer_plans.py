@@ -39,3 +39,14 @@ def test_masks_of_whole_tensors():
     """The masks in arrays are those of the reference, drawn one after another."""
     for B, C, P in ((2, 3, 1), (1, 5, 7), (2, 2, 29)):
         assert np.array_equal(plans.keep_factors(B, C, P, 0.3, -5, 1 << 40), R.keep_factors(B, C, P, 0.3, -5, 1 << 40))
+
+
+def test_long_rows_are_split():
+    """Few rows of more than 16384 positions are split whatever their length, as long as five tensors of two bytes fit in
+    288 GB and a launch has fewer than 2^32 work-items."""
+    for rows in (1, 2, 3, 17, 64, 100, 191):
+        for L in [16385] + [2 ** i + d for i in range(15, 41) for d in (-1, 0, 1)]:
+            lanes, waves, nseg = plans.scan_plan(rows, L)
+            if rows * L * 10 <= 288e9:
+                assert nseg == -(-L // 4096), (rows, L)
+            assert rows * nseg * 64 * waves < 1 << 32, (rows, L)
