@@ -244,7 +244,7 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
       if (backward && lp == 0 && widest > 0) break;
       const bool many = (groups >> lp) * B >= 512;
       if (!backward && many && (take(1, lp, 512) || take(2, lp, 512) || take(4, lp, 512))) return s;
-      if (take(1, lp, kMaxNT) || take(2, lp, kMaxNT) || take(4, lp, norm_threads(4))) return s;
+      if (take(1, lp, kMaxNT) || take(2, lp, kMaxNT)) return s;
       if (!backward && lp <= 1 && take(8, lp, norm_threads(8))) return s;
     }
   }

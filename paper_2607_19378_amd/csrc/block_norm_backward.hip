@@ -166,7 +166,7 @@ __device__ __forceinline__ float second_kind(const NormArgs& a, const Joint<3, V
 constexpr int kSumTiles = 64;
 
 template <typename TS, int V, int K, typename Has>
-__global__ void __launch_bounds__(V == 1 ? kMaxNT : norm_threads(K)) norm_backward(NormArgs a) {
+__global__ void __launch_bounds__(kMaxNT) norm_backward(NormArgs a) {
   __shared__ Joint<3, V> lds;
   __shared__ Joint<1, V> lds1;
   const Draws draws(a);
@@ -503,13 +503,13 @@ hipError_t launch(const NormArgs& a, int NT, size_t lds, hipStream_t st) {
 template <typename TS, typename Has>
 hipError_t backward_held(const NormArgs& a, const NormShape& s, hipStream_t st) {
   constexpr int V = 16 / sizeof(TS);
-  const size_t lds = a.z ? (size_t)s.K * 2 * s.V * s.NT * sizeof(float) : 0;  // at most 128 KB (norm_threads)
+  const size_t lds = a.z ? (size_t)s.K * 2 * s.V * s.NT * sizeof(float) : 0;  // at most 128 KB: two channels of eight points a thread
 #define HY_CASE(v, k) \
   if (s.V == v && s.K == k) return launch<norm_backward<TS, v, k, Has>>(a, s.NT, lds, st);
   if constexpr (!Has::TAIL) {
     HY_CASE(1, 1) HY_CASE(1, 4)
   }
-  HY_CASE(V, 1) HY_CASE(V, 2) HY_CASE(V, 4)
+  HY_CASE(V, 1) HY_CASE(V, 2)
 #undef HY_CASE
   return hipErrorInvalidValue;
 }

@@ -1,5 +1,7 @@
 """The GPU tests of the recurrence and the norms reach the plans that they are meant for: a rule that moves fails here,
 without a GPU."""
+import re
+
 import numpy as np
 import pytest
 
@@ -50,3 +52,18 @@ def test_long_rows_are_split():
             if rows * L * 10 <= 288e9:
                 assert nseg == -(-L // 4096), (rows, L)
             assert rows * nseg * 64 * waves < 1 << 32, (rows, L)
+
+
+def test_every_kernel_of_the_norms_is_chosen():
+    """The kernels in the library, by type, points a lane and channels a thread, are those that the listed calls choose."""
+    with open(plans.H.LIB_PATH, "rb") as f:
+        names = set(re.findall(rb"1[23]norm_(forward|backward)I([ft])Li(\d)ELi(\d)ENS", f.read()))
+    built = {(way == b"backward", "bf16" if t == b"t" else "f32", int(v), int(k)) for way, t, v, k in names}
+    chosen = set()
+    for dtype in ("f32", "bf16"):
+        for way in (False, True):
+            for shape in [s for s, _, _, _ in plans.NORM]:
+                V, _, K, _ = plans.norm_plan(*shape, dtype, way)
+                if K:
+                    chosen.add((way, dtype, V, K))
+    assert built == chosen
