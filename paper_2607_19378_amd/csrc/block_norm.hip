@@ -255,20 +255,30 @@ NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward) 
   return s;
 }
 
+// log2 of the consecutive tiles of an XCD's turn: 32 lanes' points, 512 bytes of a row, but
+// every XCD has a turn (1 x 2048 x 256 fp32: 12 against 17 us forward, 14 against 24 backward).
+// Samples of one tile share no lines.  Forward, up to 32 of them stay together all the same, as
+// each XCD that has one fetches the weights (32 x 1024 x 1 bf16: 3.6 us against 4.2 for one
+// after the other; 128 x 2048 x 1: 5.1 against 5.3), but no more than 256 KB of a tensor, or one
+// XCD moves too much (32 x 8192 x 1 bf16: 8.3 us against 13.1 for 32 together and 8.4 for one
+// after the other; 32 x 4096 x 1 fp32: 5.1, 6.4 and 5.2).  Backward every workgroup less is one
+// less to add up (64 x 6000 x 1 bf16: 16 against 37 us).
+uint32_t norm_log_run(int64_t sample_bytes, int64_t tiles, int64_t row_tiles, int lp, bool backward) {
+  if (row_tiles == 1 && backward) return 0;
+  int run = 5 - lp;
+  if (row_tiles == 1)
+    while (run > 0 && sample_bytes << run > 256 * 1024) --run;
+  else
+    while (run > 0 && tiles < int64_t(8) << run) --run;
+  return (uint32_t)run;
+}
+
 void norm_tiles(NormArgs& a, const NormShape& s, bool backward) {
   const int64_t points = (int64_t)s.V << s.lp, row_tiles = (a.P + points - 1) / points;
   a.lp = s.lp;
   a.row_tiles = (uint32_t)row_tiles;
   a.tiles = (uint32_t)(row_tiles * a.B);  // fewer than 2^31 + 2^26: kMaxNormPoints points, of which a tile has 4 or a row's
-  // 32 lanes' points, 512 bytes, but every XCD has a turn (1 x 2048 x 256 fp32: 12 against 17 us
-  // forward, 14 against 24 backward).  Samples of one tile share no lines; forward they stay
-  // together all the same, or each XCD fetches the weights (32 x 1024 x 1 bf16: 3.7 against
-  // 4.4 us), backward every workgroup less is one less to add up (64 x 6000 x 1 bf16: 16
-  // against 37 us).
-  const bool tokens = row_tiles == 1;
-  a.log_run = tokens && backward ? 0 : 5 - s.lp;
-  if (!tokens)
-    while (a.log_run > 0 && a.tiles < 8u << a.log_run) --a.log_run;
+  a.log_run = norm_log_run(a.C * a.P * (a.bf16 ? 2 : 4), a.tiles, row_tiles, s.lp, backward);
   const uint32_t round = a.log_run > 0 ? 8u << a.log_run : 1;
   a.turns = (a.tiles + round - 1) / round * round;
 }

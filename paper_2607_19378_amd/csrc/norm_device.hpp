@@ -308,6 +308,7 @@ struct NormShape {
 // threads of a workgroup at most, so that K channels a thread stay in registers
 constexpr int norm_threads(int K) { return K > 2 ? 512 : 1024; }
 NormShape norm_shape(int64_t C, int64_t P, int64_t B, bool bf16, bool backward);
+uint32_t norm_log_run(int64_t sample_bytes, int64_t tiles, int64_t row_tiles, int lp, bool backward);
 void norm_tiles(NormArgs& a, const NormShape& s, bool backward);
 
 }  // namespace hyenand

@@ -67,3 +67,10 @@ def keep_factors(B, C, P, p, seed, offset):
         k = [(k[0] + R._W[0]) & 0xFFFFFFFF, (k[1] + R._W[1]) & 0xFFFFFFFF]
     bits = np.stack([w for x in c for w in (x & np.uint64(0xFFFF), x >> np.uint64(16))], -1)
     return (bits.reshape(B, C, groups * 8)[..., :P] >= drop) * (65536.0 / (65536 - drop))
+
+
+def norm_run(sample_bytes, tiles, row_tiles, lp, backward):
+    """Consecutive tiles of an XCD's turn, of norm_log_run."""
+    fn = H.lib()._ZN7hyenand12norm_log_runElllib
+    fn.argtypes, fn.restype = [ctypes.c_int64] * 3 + [ctypes.c_int, ctypes.c_bool], ctypes.c_uint32
+    return 1 << fn(sample_bytes, tiles, row_tiles, lp, backward)

@@ -67,3 +67,13 @@ def test_every_kernel_of_the_norms_is_chosen():
                 if K:
                     chosen.add((way, dtype, V, K))
     assert built == chosen
+
+
+def test_wide_samples_of_one_tile_go_to_several_xcds():
+    """An XCD's turn is at most 256 KB of a tensor, or one sample; small ones stay together."""
+    for B, C, size, run in ((32, 1024, 2, 32), (32, 4096, 2, 32), (32, 8192, 2, 16), (64, 6000, 2, 16), (64, 2048, 4, 32),
+                            (32, 4096, 4, 16), (16, 8192, 4, 8), (4, 1 << 20, 2, 1), (1, 1 << 25, 4, 1)):
+        assert plans.norm_run(C * size, B, 1, 0, False) == run
+        assert plans.norm_run(C * size, B, 1, 0, True) == 1
+    assert plans.norm_run(1 << 24, 1 << 14, 64, 2, False) == plans.norm_run(1 << 24, 1 << 14, 64, 2, True) == 8
+    assert plans.norm_run(1 << 21, 8, 8, 3, True) == 1  # every XCD has a tile
