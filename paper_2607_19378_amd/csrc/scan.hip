@@ -157,38 +157,49 @@ hipError_t forward(const ScanArgs& a, const ScanShape& p, hipStream_t s) {
 }
 
 constexpr int kStepNT = 256;
+constexpr int kStepLook = 8 * kStepNT;  // rows looked at before the workgroup compares
 
 // One position of every sequence, a thread a channel.  Rows with the same slot
 // are positions of one sequence, in the order of the batch: the workgroup of the
-// first of them takes all, those of the others end.
+// first of them takes all, those of the others end.  A search of the batch ends
+// with the first kStepLook rows that hold the slot: searches through all of it cost
+// the square of the rows with one state (16384 of them: 1220 ms, now 12).
 template <typename TS>
 __global__ void __launch_bounds__(kStepNT) scan_step(ScanStepArgs a) {
-  __shared__ int earlier, next;
-  int64_t b = blockIdx.y;
-  const int c = blockIdx.x * kStepNT + threadIdx.x;
+  __shared__ int first[2][kStepNT / 64];
+  int b = blockIdx.y, turn = 0;
+  const int c = blockIdx.x * kStepNT + threadIdx.x, B = (int)a.B;
   const int64_t slot = a.slots ? a.slots[b] : b;
   const bool in_pool = slot >= 0 && slot < a.nslots;
-  int later = (int)a.B;
-  if (a.slots) {
-    if (threadIdx.x == 0) {
-      earlier = 0;
-      next = (int)a.B;
-    }
-    __syncthreads();
-    if (in_pool)
-      for (int i = threadIdx.x; i < a.B; i += kStepNT)
-        if (a.slots[i] == slot && i != b) {
-          if (i < b) earlier = 1;
-          else atomicMin(&next, i);
-        }
-    __syncthreads();
-    if (earlier) return;
-    later = next;
+  // the first of the rows from ... to, but for row b, with this slot (B: none)
+  auto look = [&](int from, int to) {
+    int mine = B;
+    for (int i = from + (int)threadIdx.x; i < to; i += kStepNT)
+      if (a.slots[i] == slot && i != b) mine = min(mine, i);
+    if (__ballot(mine < B))
+      for (int d = 32; d > 0; d /= 2) mine = min(mine, __shfl_xor(mine, d));
+    if ((threadIdx.x & 63) == 0) first[turn][threadIdx.x >> 6] = mine;
+    __syncthreads();  // (and the results of the look before the last one have been read)
+    int found = B;
+#pragma unroll
+    for (int w = 0; w < kStepNT / 64; ++w) found = min(found, first[turn][w]);
+    turn ^= 1;
+    return found;
+  };
+  auto search = [&](int from) {
+    int found = B;
+    for (; from < B && found == B; from += kStepLook) found = look(from, min(from + kStepLook, B));
+    return found;
+  };
+  int later = B;
+  if (a.slots && in_pool) {
+    later = search(0);
+    if (later < b) return;
   }
   float h = in_pool && c < a.C ? a.state[slot * a.C + c] : 0.f;
   for (;;) {
     if (c < a.C) {
-      const int64_t i = b * a.C + c;
+      const int64_t i = (int64_t)b * a.C + c;
       float y = 0.f;
       if (in_pool) {
         const float e = pow2f(decay(ld1(reinterpret_cast<const TS*>(a.la) + i)));
@@ -198,16 +209,10 @@ __global__ void __launch_bounds__(kStepNT) scan_step(ScanStepArgs a) {
       }
       st1(reinterpret_cast<TS*>(a.y) + i, y);
     }
-    if (later >= a.B) break;
-    // the row after this one with the same slot, if there is one more
+    if (later >= B) break;
     b = later;
-    __syncthreads();
-    if (threadIdx.x == 0) next = (int)a.B;
-    __syncthreads();
-    for (int i = (int)b + 1 + threadIdx.x; i < a.B; i += kStepNT)
-      if (a.slots[i] == slot) atomicMin(&next, i);
-    __syncthreads();
-    later = next;
+    later = look(b + 1, min(b + 1 + kStepNT, B));  // (neighbours, most often)
+    if (later == B) later = search(b + 1 + kStepNT);
   }
   if (in_pool && c < a.C) a.state[slot * a.C + c] = h;
 }

@@ -489,3 +489,40 @@ def test_one_row_of_very_many_segments():
             p, q = p[..., inner].float(), q[..., cut][..., inner].float()
             assert float((p - q).norm() / p.norm()) < 4e-3
     assert torch.allclose(last, lc, rtol=1e-4)
+
+
+@pytest.mark.parametrize("B,C,N", [(2047, 3, 1), (2049, 300, 2), (5000, 5, 7), (5000, 2, 3000), (65535, 3, 1)])
+def test_slots_named_many_times(B, C, N):
+    """Rows of one state all over a batch, next to each other and far apart: each state is a sequence of the recurrence, and
+    the largest batch on one state takes no second of the GPU's time."""
+    import torch
+    from paper_2607_19378_amd import hyenand as H
+    rng = np.random.default_rng(B + N)
+    x1, x2, v = (rng.standard_normal((B, C)).astype(np.float32) for _ in range(3))
+    la, D = -rng.uniform(0.5, 1, (B, C)).astype(np.float32), rng.standard_normal(C).astype(np.float32)
+    slots, state = rng.integers(0, N, B), rng.standard_normal((N, C)).astype(np.float32)
+    if N > 2:
+        slots[slots == 1] = N + 4  # idle rows among the others
+    dev = [on_gpu(t) for t in (x1, x2, v, la, D, state)]
+    pool, where = dev[5], on_gpu(slots)
+    log(f"[scan] slots named many times B={B} C={C} N={N}")
+    H.scan_step(*dev[:5], pool.clone(), where)
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    begin.record()
+    y = H.scan_step(*dev[:5], pool, where)
+    end.record()
+    torch.cuda.synchronize()
+    assert begin.elapsed_time(end) < 1000
+    y, pool = from_device(y), from_device(pool)
+    assert np.all(y[slots >= N] == 0)
+    for s in range(N):
+        rows = np.flatnonzero(slots == s)
+        if rows.size == 0:
+            assert np.array_equal(pool[s], state[s])
+            continue
+        args = [np.ascontiguousarray(t[rows].T)[None].astype(np.float64) for t in (x1, x2, v, la)] + [D.astype(np.float64)]
+        ref, mag = R.scan(*args, h0=state[s:s + 1]), R.scan_magnitudes(*args, h0=state[s:s + 1])
+        # two roundings and an exponential's a step, each older one by exp(-1/2) less: 3 / (1 - exp(-1/2)), and four of y
+        tol = (3 / (1 - np.exp(-0.5)) + 4) * 2.0 ** -23
+        assert np.all(np.abs(y[rows].T - ref["y"][0]) <= tol * mag["y"][0] + 1e-37), s
+        assert np.all(np.abs(pool[s] - ref["h_last"][0]) <= tol * mag["h_last"][0] + 1e-37), s
