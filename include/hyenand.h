@@ -539,6 +539,7 @@ hyenand_status hyenand_scan_step(const void* x1, const void* x2, const void* v, 
  *
  * x, z, gate, x_out, n : contiguous [B, C, P] of dtype; w_post, scale, w_pre: [C]
  *   of dtype; all aligned to their element.  gate NULL: no gate.  scale NULL: 1.
+ *   A branch z always has its norm: w_post is given with it.
  * First block: z, gate, w_post, scale and x_out NULL, dropout_p 0: n of x alone.
  * Last block: w_pre and n NULL: x_out alone.
  * Drop: each point is dropped (0) with the probability dropout_p (0 <= dropout_p
@@ -573,7 +574,8 @@ hyenand_status hyenand_block_norm(const void* x, const void* z, const void* gate
  * of the forward's x and, with z, of the whole sum: both have the same one.
  * A point whose norm was 0 by a root of 0 passes no gradient through it.
  * workspace: at least hyenand_block_norm_backward_workspace_size() bytes, 16-byte
- * aligned.  The weights' gradients are added up in a fixed order.
+ * aligned.  The weights' gradients are added up in a fixed order, in fp32 over 64
+ * tiles of points at most and in 64 bits from there.
  */
 hyenand_status hyenand_block_norm_backward(const void* x_out, const void* z, const void* gate, const void* w_post,
                                            const void* scale, const void* w_pre, float eps_post, float eps_pre,

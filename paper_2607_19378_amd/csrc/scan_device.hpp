@@ -130,10 +130,12 @@ __device__ __forceinline__ int64_t row_length(const ScanArgs& a, int64_t row) {
 }
 
 // Segments of a split row are taken by workgroups of one launch, each of which
-// reads its inputs once and holds them while it learns the state that enters it.
+// reads its inputs once and holds them while it learns the state that enters it: a
+// prefix in a single pass with look-back (Merrill and Garland, "Single-pass Parallel
+// Prefix Scan with Decoupled Look-back", 2016).
 // A workgroup draws its segment from its row's counter, so that every segment before
-// its own in the row is finished or being worked on.  It publishes what its segment does to a state (its span) before it waits for
-// anything, then looks for the nearest segment before it that has published the
+// its own in the row is finished or being worked on.  It publishes what its segment
+// does to a state (its span) before it waits for anything, then looks for the nearest segment before it that has published the
 // state behind it, and takes the spans between from there on in their order, so
 // that the roundings do not depend on the timing.  Each wait ends: a row's first
 // segment waits for nothing, and each other one for segments that are being worked on.

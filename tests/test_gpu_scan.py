@@ -98,7 +98,7 @@ def test_short_rows(L, dtype):
     run_case(3, 37, L, dtype, L, packed=L % 2 == 1, lengths=True, carry=True)
 
 
-# four wavefronts a row, then sixteen, with tiles that end inside, at and behind a block
+# four wavefronts a row, from five tiles on eight, with tiles that end inside, at and behind a block
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("L", [257, 511, 512, 513, 1025, 1501, 2048, 2049, 4095, 8192, 8193, 9001])
 def test_long_rows(L, dtype):
@@ -110,14 +110,14 @@ def test_packed_rows(L):
     run_case(2, 5, L, "f32", L, packed=True, lengths=False, carry=False)
 
 
-# one wavefront a row from 2048 rows on, four from 512 on
+# four wavefronts a row, and eight below 1024 rows
 @pytest.mark.parametrize("B,C,L", [(4, 515, 600), (3, 700, 1300), (2, 300, 2700), (1, 513, 4100)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_many_rows(B, C, L, dtype):
     run_case(B, C, L, dtype, C, packed=True, lengths=True, carry=True)
 
 
-# rows split into segments: the last one shorter, and a sample that ends in each of them
+# the longest row of one piece, then rows split into segments: the last one shorter, and a sample that ends in each
 @pytest.mark.parametrize("B,C,L", [(1, 1, 16384), (1, 3, 40000), (5, 2, 33333), (2, 50, 17001)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_split_rows(B, C, L, dtype):
