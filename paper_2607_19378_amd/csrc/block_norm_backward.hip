@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(1024) norm_weights(NormArgs a) {
   double x = 0.0, y = 0.0;
   if (c < a.C)
 #pragma unroll 8
-    for (int i = part; i < a.groups * a.rows; i += 32) {  // (fewer than 2^26)
+    for (int i = part; i < a.all_rows; i += 32) {
       const float2 w = a.partial[(int64_t)i * a.C + c];
       x += w.x;
       y += w.y;
@@ -551,12 +551,13 @@ NormShape plan(NormArgs& a) {
   a.groups = groups_of(a, s);
   const uint32_t each = (a.turns + a.groups - 1) / a.groups;
   a.rows = (int)((each + kSumTiles - 1) / kSumTiles);
+  a.all_rows = a.groups * a.rows;  // fewer than 2^26
   a.parts = 0;
   if (s.K == 0) split_parts(a, s);
   return s;
 }
 
-size_t partial_bytes(const NormArgs& a) { return (size_t)a.groups * (size_t)a.rows * (size_t)a.C * sizeof(float2); }
+size_t partial_bytes(const NormArgs& a) { return (size_t)a.all_rows * (size_t)a.C * sizeof(float2); }
 
 }  // namespace
 

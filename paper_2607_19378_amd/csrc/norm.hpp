@@ -26,7 +26,8 @@ struct NormArgs {
   uint32_t tiles, row_tiles;        // tiles of points in all, and of a sample
   uint32_t log_run;                 // log2 of the consecutive tiles of an XCD's turn
   uint32_t turns;                   // tiles, and the turns that fall behind the last one
-  int groups, rows;                 // workgroups of the backward (of a part of the channels), and rows of their sums
+  int groups;                       // workgroups of the backward (of a part of the channels)
+  int rows, all_rows;               // rows of sums of each workgroup, and of all
   int part, parts;                  // split calls: channels of a part, and parts
   float* sums;                      // [tiles, parts, sums of a point, points]
 };
