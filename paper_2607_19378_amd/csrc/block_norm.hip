@@ -203,13 +203,13 @@ hipError_t forward(const NormArgs& a, const NormShape& s, hipStream_t st) {
 
 // A row's accesses are as wide as 8 lanes make them (128 bytes), since narrower
 // ones cost most (8 x 256 x 64 x 64 fp32 forward: 40 us at 128 bytes, 45, 48 and 61 us
-// at 64, 32 and 16; backward of 2 x 512 x 8192 bf16: 50 us at 64 bytes, 73 and 85 us
+// at 64, 32 and 16; backward of 2 x 512 x 8192 bf16: 47 us at 64 bytes, 56 and 73 us
 // at 32 and 16), as far as the channels then fit.  The forward takes four channels a
 // thread in 512 threads where two would need 1024 (2 x 512 x 8192 bf16: 21 against
 // 24 us, two workgroups a CU), unless that leaves CUs without a tile; eight only
 // where four would halve the width to 16 bytes (2 x 2048 x 2048 bf16: 30 against
 // 34 us; 2 x 512 x 8192: 27 against 21 us for 128 bytes in place of 64).  The backward
-// takes as few channels a thread as fit (2 x 512 x 8192 bf16: 50 us with two, 56 us
+// takes as few channels a thread as fit (2 x 512 x 8192 bf16: 47 us with two, 50 us
 // with four), and gives up tiles of 16 bytes for two sweeps (norm_sums).
 // Rows shorter than a lane's 16 bytes are one point a lane; four channels a thread where
 // threads of one would fill the chip (2^19 of them; 4096 x 1024 x 1 bf16: forward 21 against 53

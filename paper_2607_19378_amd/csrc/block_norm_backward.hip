@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kMaxNT) norm_backward(NormArgs a) {
 // Where a tile of 32 bytes or more of a row does not fit in registers, the tensors
 // are read twice in place of once: norm_sums leaves each point's sums over a part of
 // the channels, norm_apply joins them and does the rest.  (2 x 2048 x 2048 bf16: 59 us
-// against 81 us for tiles of 16 bytes in registers; 2 x 1024 x 4095 bf16: 97 us against 74 us
+// against 78 us for tiles of 16 bytes in registers; 2 x 1024 x 4095 bf16: 97 us against 75 us
 // for tiles of 32 bytes in registers, so only tiles of 16 bytes are given up.)  gmw is linear in gx_out, gn and
 // x, so its sum with t follows from three more sums of the first sweep:
 //   sum gmw t = sum w t gx_out + q sum w t gn w_pre - q^3 mean(gn w_pre x) sum w t x,
